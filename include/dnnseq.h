@@ -1,0 +1,161 @@
+/*
+ * dnnseq.h - C ABI of the operators of sequence models on 16-bit tensors on one AMD MI355X
+ * (gfx950), exported by the same shared library as mbconv.h and dnnops.h: attention (forward, the
+ * form for single tokens over long caches, backward), linear layers (matrix product with bias,
+ * activation and residual; backward) and layer normalisation (forward, backward).
+ *
+ * Conventions
+ *   - Tensors hold bf16 or fp16 (one type in a call); vectors beside them (bias, gamma, beta, mean,
+ *     rstd, lse and their gradients) hold fp32.  Products, sums, softmax and row statistics are
+ *     taken in fp32; results are rounded once, to nearest even.
+ *   - Strides are in elements; the last dimension is contiguous.  Every pointer is a DEVICE pointer
+ *     owned by the caller and must be 16-byte aligned.  Outputs must not overlap inputs or each
+ *     other unless the call says so.
+ *   - Scratch: at least the number of bytes that the call's *_scratch_bytes gives, overwritten;
+ *     NULL where that is 0.  Calls that overlap in time need scratch of their own.
+ *   - The library allocates nothing, keeps no state and never synchronises: all work is enqueued
+ *     on the hipStream_t passed as `hip_stream` (NULL = the default stream), without memset nodes,
+ *     so calls can be captured into a graph.
+ *   - Every argument check happens on the host before the first launch and returns a negative
+ *     status without touching device memory.  A failed launch returns DNNSEQ_EHIP.  No call throws
+ *     or aborts.
+ *   - Reductions run in a fixed order without floating-point atomics: results are bitwise
+ *     repeatable.
+ */
+#ifndef DNNSEQ_H
+#define DNNSEQ_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum {
+    DNNSEQ_OK = 0,
+    DNNSEQ_EINVAL = -1,       /* NULL pointer, bad size, stride, enumerator or scale */
+    DNNSEQ_EUNSUPPORTED = -2, /* sizes beyond what the kernels take (see each operator) */
+    DNNSEQ_ESCRATCH = -3,     /* the shape needs scratch and none was passed */
+    DNNSEQ_EALIGN = -4,       /* pointer not 16-byte aligned */
+    DNNSEQ_EHIP = -5          /* a launch failed */
+} dnnseq_status;
+
+typedef enum { DNNSEQ_BF16 = 0, DNNSEQ_FP16 = 1 } dnnseq_dtype;
+
+/* ---- attention -------------------------------------------------------------------------------
+ * For every request b and query head h (key head g = h / (q_heads/kv_heads)):
+ *   s[i][j] = scale * q[i] . k[j],  p = softmax of s over the visible keys j,  o[i] = sum_j p[i][j] v[j]
+ *   lse[i]  = log sum_j exp(s[i][j])
+ * Key j is visible to query i when i < ql, j < kl and, with `causal`, j <= i + kl - ql, where ql and
+ * kl are the request's lengths (q_lens[b], kv_lens[b], or q_len and kv_len where those are NULL;
+ * values outside [0, q_len] and [0, kv_len] are clamped).  A query that sees no key gives o = 0,
+ * lse = -infinity and takes no part in any gradient.  Rows of q, k, v and dout at or past a request's
+ * lengths may hold anything (NaN and infinity as well) and do not reach any result; rows of o, dq,
+ * dk and dv there are written as zeros.
+ *
+ * head_dim: a multiple of 8, at most DNNSEQ_MAX_HEAD_DIM.  q_heads is a multiple of kv_heads.
+ * q_len, kv_len and batch may be 0.  Strides (batch, head, token) are multiples of 8 elements, not
+ * negative; for k, v, q and dout they may be 0 (broadcast), for the outputs the elements must not
+ * overlap. */
+#define DNNSEQ_MAX_HEAD_DIM 128
+
+typedef struct {
+    int64_t batch, head, token;
+} dnnseq_stride;
+
+typedef struct {
+    int32_t dtype; /* dnnseq_dtype */
+    int32_t batch, q_heads, kv_heads, q_len, kv_len, head_dim;
+    int32_t causal; /* 0 or 1 */
+    float scale;    /* positive, finite */
+    dnnseq_stride q, k, v, o;
+    dnnseq_stride dout, dq, dk, dv; /* backward only */
+} dnnseq_attention_desc;
+
+/* Host-only; 0 for a descriptor that the call would refuse. */
+size_t dnnseq_attention_forward_scratch_bytes(const dnnseq_attention_desc *d);
+size_t dnnseq_attention_backward_scratch_bytes(const dnnseq_attention_desc *d);
+
+/* lse (may be NULL): fp32 [batch][q_heads][q_len], contiguous; the backward call needs it.
+ * q_lens, kv_lens (may be NULL): int32 [batch] on the device. */
+dnnseq_status dnnseq_attention_forward(const dnnseq_attention_desc *d, const void *q, const void *k, const void *v,
+                                       const int32_t *q_lens, const int32_t *kv_lens, void *o, float *lse,
+                                       void *scratch, void *hip_stream);
+
+/* Gradients of sum(o * dout); o and lse are the forward call's.  The probabilities are computed
+ * again from q, k and lse.  dk and dv sum over the query heads that share a key head. */
+dnnseq_status dnnseq_attention_backward(const dnnseq_attention_desc *d, const void *q, const void *k, const void *v,
+                                        const void *o, const void *dout, const float *lse, const int32_t *q_lens,
+                                        const int32_t *kv_lens, void *dq, void *dk, void *dv, void *scratch,
+                                        void *hip_stream);
+
+/* ---- linear ----------------------------------------------------------------------------------
+ *   z[m][n] = sum_k x[m][k] w[n][k] + bias[n],   y = act(z) + residual
+ * Rows of the matrices are ld* elements apart (at least their length, a multiple of 8, below 2^22).
+ * n and k: multiples of 8.  m may be 0. */
+typedef enum {
+    DNNSEQ_ACT_NONE = 0,
+    DNNSEQ_ACT_RELU = 1,
+    DNNSEQ_ACT_GELU = 2, /* z/2 (1 + erf(z/sqrt 2)) */
+    DNNSEQ_ACT_SILU = 3,
+    DNNSEQ_ACT_MISH = 4
+} dnnseq_activation;
+
+typedef struct {
+    int32_t dtype;      /* dnnseq_dtype */
+    int32_t activation; /* dnnseq_activation */
+    int32_t m, n, k;
+    int32_t dw_fp32; /* 1: dw is fp32, 0: dw has the tensors' type */
+    int64_t ldx, ldw, ldy, ldresidual, ldz;
+    int64_t lddy, lddx, lddx_add, lddw; /* backward only */
+} dnnseq_linear_desc;
+
+size_t dnnseq_linear_forward_scratch_bytes(const dnnseq_linear_desc *d);
+size_t dnnseq_linear_backward_scratch_bytes(const dnnseq_linear_desc *d);
+
+/* bias: fp32 [n] or NULL.  residual: [m][n] or NULL; y may be the same buffer (with ldy equal to
+ * ldresidual).  z: where to keep z (rounded to the tensors' type) for the backward call, or NULL. */
+dnnseq_status dnnseq_linear_forward(const dnnseq_linear_desc *d, const void *x, const void *w, const float *bias,
+                                    const void *residual, void *y, void *z, void *scratch, void *hip_stream);
+
+/* With g = dy * act'(z) (z is read only where there is an activation, and may be NULL otherwise):
+ *   dx[m][k] = sum_n g[m][n] w[n][k] + dx_add[m][k],  dw[n][k] = sum_m g[m][n] x[m][k],  db[n] = sum_m g[m][n]
+ * (all overwritten).  dx, dw and db may each be NULL: what is not asked for is not computed.
+ * dx_add (may be NULL): a gradient that reaches x on another path; dx may be the same buffer (with
+ * lddx equal to lddx_add).  The gradient of the residual is dy itself. */
+dnnseq_status dnnseq_linear_backward(const dnnseq_linear_desc *d, const void *x, const void *w, const void *z,
+                                     const void *dy, const void *dx_add, void *dx, void *dw, float *db,
+                                     void *scratch, void *hip_stream);
+
+/* ---- layer normalisation -----------------------------------------------------------------------
+ * Each row of x[rows][cols]: y = gamma*(x - mean)*rstd + beta, mean and rstd = 1/sqrt(var + eps) with
+ * the biased variance.  Rows are ld* elements apart (any distance of at least cols).  cols: at most
+ * DNNSEQ_MAX_NORM_COLS.  rows may be 0. */
+#define DNNSEQ_MAX_NORM_COLS 16384
+
+typedef struct {
+    int32_t dtype; /* dnnseq_dtype */
+    int32_t rows, cols;
+    float eps; /* >= 0, finite */
+    int64_t ldx, ldy;
+    int64_t lddy, lddx, lddx_add; /* backward only */
+} dnnseq_layernorm_desc;
+
+size_t dnnseq_layernorm_backward_scratch_bytes(const dnnseq_layernorm_desc *d);
+
+/* gamma, beta: fp32 [cols].  mean, rstd: fp32 [rows], written for the backward call.  y may be the
+ * same buffer as x (with ldy equal to ldx) where no backward call follows. */
+dnnseq_status dnnseq_layernorm_forward(const dnnseq_layernorm_desc *d, const void *x, const float *gamma,
+                                       const float *beta, void *y, float *mean, float *rstd, void *hip_stream);
+
+/* dx (+ dx_add, may be NULL: the gradient that reaches x past the normalisation; dx may be the same
+ * buffer, with lddx equal to lddx_add), dgamma[c] = sum_r dy*xhat, dbeta[c] = sum_r dy, fp32. */
+dnnseq_status dnnseq_layernorm_backward(const dnnseq_layernorm_desc *d, const void *x, const void *dy,
+                                        const float *gamma, const float *mean, const float *rstd, const void *dx_add,
+                                        void *dx, float *dgamma, float *dbeta, void *scratch, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DNNSEQ_H */

@@ -11,8 +11,10 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmbconv.so")
 SOURCES = ["mbconv_api.hip", "kernels_gemm.hip", "kernels_big.hip", "kernels_bf.hip", "kernels_bw.hip", "kernels_x3.hip", "kernels_xk.hip", "kernels_bwd1x1.hip", "kernels_wgr.hip", "kernels_evx.hip", "kernels_wave.hip", "kernels_pv16.hip", "kernels_dw.hip", "kernels_dw4.hip", "kernels_dw2.hip", "kernels_dwr.hip", "kernels_misc.hip"]
-# sources without a block activation (Mish, layer normalisation, softmax): compiled once
-SOURCES_ONCE = ["kernels_ops.hip"]
+# sources without a block activation (Mish, layer normalisation, softmax; the 16-bit sequence
+# operators): compiled once
+SOURCES_ONCE = ["kernels_attn_bwd.hip", "kernels_attn.hip", "kernels_linear.hip", "kernels_norm.hip", "dnnseq_api.hip",
+                "kernels_ops.hip"]
 # packed fp32 VALU ops are disabled for the device pass (the host pass does not know the
 # feature and says so; harmless)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
@@ -30,7 +32,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     hipcc = _hipcc()
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    headers.append(os.path.join(HERE, "..", "include", "mbconv.h"))
+    headers += [os.path.join(HERE, "..", "include", h) for h in ("mbconv.h", "dnnops.h", "dnnseq.h")]
     newest_hdr = max(os.path.getmtime(h) for h in headers)
 
     def compile_one(job) -> str:

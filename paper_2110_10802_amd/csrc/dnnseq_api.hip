@@ -1,0 +1,264 @@
+// C ABI of the 16-bit sequence operators: argument checks (host only, before any launch).
+#include "dnnseq_launch.h"
+
+#include <cmath>
+#include <initializer_list>
+
+namespace {
+
+bool bad_align(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if ((uintptr_t)p & 15)
+            return true;
+    return false;
+}
+bool any_null(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (!p)
+            return true;
+    return false;
+}
+dnnseq_status status(hipError_t e) { return e == hipSuccess ? DNNSEQ_OK : DNNSEQ_EHIP; }
+
+// ---- attention
+bool stride_ok(const dnnseq_stride &s)
+{
+    return s.batch >= 0 && s.head >= 0 && s.token >= 0 && s.batch % 8 == 0 && s.head % 8 == 0 && s.token % 8 == 0;
+}
+
+// Whether no two elements of a tensor share an address: with its dimensions in the order of their
+// strides, each has to pass over the whole extent of those below it.
+bool disjoint(const dnnseq_stride &s, int64_t batch, int64_t heads, int64_t len, int64_t dim)
+{
+    int64_t st[3] = {s.batch, s.head, s.token}, n[3] = {batch, heads, len};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (st[j] > st[j + 1]) {
+                const int64_t a = st[j], b = n[j];
+                st[j] = st[j + 1], n[j] = n[j + 1];
+                st[j + 1] = a, n[j + 1] = b;
+            }
+    int64_t extent = dim;
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1) {
+            if (st[i] < extent)
+                return false;
+            extent += st[i] * (n[i] - 1);
+        }
+    return true;
+}
+
+constexpr int64_t kMaxStride = (int64_t)1 << 40;      // times any 32-bit index within 63 bits
+constexpr int64_t kMaxTokenStride = (int64_t)1 << 22; // a tile's rows within 31 bits of bytes
+
+dnnseq_status check_attention(const dnnseq_attention_desc *d, bool backward)
+{
+    if (!d || (d->dtype != DNNSEQ_BF16 && d->dtype != DNNSEQ_FP16) || d->batch < 0 || d->q_heads < 1 ||
+        d->kv_heads < 1 || d->q_len < 0 || d->kv_len < 0 || d->head_dim < 1 || (d->causal != 0 && d->causal != 1) ||
+        !(d->scale > 0.f) || !std::isfinite(d->scale) || d->q_heads % d->kv_heads)
+        return DNNSEQ_EINVAL;
+    const dnnseq_stride *all[8] = {&d->q, &d->k, &d->v, &d->o, &d->dout, &d->dq, &d->dk, &d->dv};
+    for (int i = 0; i < (backward ? 8 : 4); ++i)
+        if (!stride_ok(*all[i]))
+            return DNNSEQ_EINVAL;
+    if (!disjoint(d->o, d->batch, d->q_heads, d->q_len, d->head_dim))
+        return DNNSEQ_EINVAL;
+    if (backward && (!disjoint(d->dq, d->batch, d->q_heads, d->q_len, d->head_dim) ||
+                     !disjoint(d->dk, d->batch, d->kv_heads, d->kv_len, d->head_dim) ||
+                     !disjoint(d->dv, d->batch, d->kv_heads, d->kv_len, d->head_dim)))
+        return DNNSEQ_EINVAL;
+    if (d->head_dim % 8 || d->head_dim > DNNSEQ_MAX_HEAD_DIM || d->q_len > (1 << 28) || d->kv_len > (1 << 28) ||
+        (int64_t)d->batch * d->q_heads > 65535)
+        return DNNSEQ_EUNSUPPORTED;
+    for (int i = 0; i < (backward ? 8 : 4); ++i)
+        if (all[i]->batch > kMaxStride || all[i]->head > kMaxStride || all[i]->token >= kMaxTokenStride)
+            return DNNSEQ_EUNSUPPORTED;
+    return DNNSEQ_OK;
+}
+
+// ---- linear
+bool ld_ok(int64_t ld, int cols) { return ld >= cols && ld % 8 == 0; }
+
+dnnseq_status check_linear(const dnnseq_linear_desc *d)
+{
+    if (!d || (d->dtype != DNNSEQ_BF16 && d->dtype != DNNSEQ_FP16) || d->activation < DNNSEQ_ACT_NONE ||
+        d->activation > DNNSEQ_ACT_MISH || d->m < 0 || d->n < 1 || d->k < 1 || !ld_ok(d->ldx, d->k) ||
+        !ld_ok(d->ldw, d->k) || (d->dw_fp32 != 0 && d->dw_fp32 != 1))
+        return DNNSEQ_EINVAL;
+    if (d->n % 8 || d->k % 8 || d->ldx >= (1 << 22) || d->ldw >= (1 << 22) || d->m > (1 << 28))
+        return DNNSEQ_EUNSUPPORTED;
+    return DNNSEQ_OK;
+}
+
+dnnseq_status check_ld(int64_t ld, int cols)
+{
+    return !ld_ok(ld, cols) ? DNNSEQ_EINVAL : ld >= (1 << 22) ? DNNSEQ_EUNSUPPORTED : DNNSEQ_OK;
+}
+
+// ---- layer normalisation
+dnnseq_status check_norm(const dnnseq_layernorm_desc *d, bool backward, bool add)
+{
+    if (!d || (d->dtype != DNNSEQ_BF16 && d->dtype != DNNSEQ_FP16) || d->rows < 0 || d->cols < 1 || !(d->eps >= 0.f) ||
+        !std::isfinite(d->eps) || d->ldx < d->cols || (!backward && d->ldy < d->cols) ||
+        (backward && (d->lddy < d->cols || d->lddx < d->cols)) || (add && d->lddx_add < d->cols))
+        return DNNSEQ_EINVAL;
+    const int64_t top = kMaxStride;
+    if (d->cols > DNNSEQ_MAX_NORM_COLS || d->rows > (1 << 28) || d->ldx > top || (!backward && d->ldy > top) ||
+        (backward && (d->lddy > top || d->lddx > top)) || (add && d->lddx_add > top))
+        return DNNSEQ_EUNSUPPORTED;
+    return DNNSEQ_OK;
+}
+
+} // namespace
+
+#define CHECK(e)                                                                                                       \
+    do {                                                                                                               \
+        const dnnseq_status s_ = (e);                                                                                  \
+        if (s_ != DNNSEQ_OK)                                                                                           \
+            return s_;                                                                                                 \
+    } while (0)
+
+extern "C" {
+
+size_t dnnseq_attention_forward_scratch_bytes(const dnnseq_attention_desc *d)
+{
+    return check_attention(d, false) == DNNSEQ_OK ? dsq::attention_forward_scratch(*d) : 0;
+}
+
+size_t dnnseq_attention_backward_scratch_bytes(const dnnseq_attention_desc *d)
+{
+    return check_attention(d, true) == DNNSEQ_OK ? dsq::attention_backward_scratch(*d) : 0;
+}
+
+dnnseq_status dnnseq_attention_forward(const dnnseq_attention_desc *d, const void *q, const void *k, const void *v,
+                                       const int32_t *q_lens, const int32_t *kv_lens, void *o, float *lse,
+                                       void *scratch, void *hip_stream)
+{
+    CHECK(check_attention(d, false));
+    if (!d->batch || !d->q_len)
+        return DNNSEQ_OK;
+    if (any_null({q, o}) || (d->kv_len && any_null({k, v})))
+        return DNNSEQ_EINVAL;
+    if (bad_align({q, k, v, o, lse, q_lens, kv_lens, scratch}))
+        return DNNSEQ_EALIGN;
+    if (dsq::attention_forward_scratch(*d) && !scratch)
+        return DNNSEQ_ESCRATCH;
+    return status(
+        dsq::launch_attention_forward(*d, q, k, v, q_lens, kv_lens, o, lse, scratch, (hipStream_t)hip_stream));
+}
+
+dnnseq_status dnnseq_attention_backward(const dnnseq_attention_desc *d, const void *q, const void *k, const void *v,
+                                        const void *o, const void *dout, const float *lse, const int32_t *q_lens,
+                                        const int32_t *kv_lens, void *dq, void *dk, void *dv, void *scratch,
+                                        void *hip_stream)
+{
+    CHECK(check_attention(d, true));
+    if (!d->batch || (!d->q_len && !d->kv_len))
+        return DNNSEQ_OK;
+    if ((d->q_len && any_null({q, o, dout, lse, dq})) || (d->kv_len && any_null({k, v, dk, dv})))
+        return DNNSEQ_EINVAL;
+    if (bad_align({q, k, v, o, dout, lse, q_lens, kv_lens, dq, dk, dv, scratch}))
+        return DNNSEQ_EALIGN;
+    if (dsq::attention_backward_scratch(*d) && !scratch)
+        return DNNSEQ_ESCRATCH;
+    return status(dsq::launch_attention_backward(*d, q, k, v, o, dout, lse, q_lens, kv_lens, dq, dk, dv, scratch,
+                                                 (hipStream_t)hip_stream));
+}
+
+size_t dnnseq_linear_forward_scratch_bytes(const dnnseq_linear_desc *d)
+{
+    return check_linear(d) == DNNSEQ_OK && d->m ? dsq::linear_forward_scratch(*d) : 0;
+}
+
+size_t dnnseq_linear_backward_scratch_bytes(const dnnseq_linear_desc *d)
+{
+    return check_linear(d) == DNNSEQ_OK ? dsq::linear_backward_scratch(*d) : 0;
+}
+
+dnnseq_status dnnseq_linear_forward(const dnnseq_linear_desc *d, const void *x, const void *w, const float *bias,
+                                    const void *residual, void *y, void *z, void *scratch, void *hip_stream)
+{
+    CHECK(check_linear(d));
+    CHECK(check_ld(d->ldy, d->n));
+    if (residual)
+        CHECK(check_ld(d->ldresidual, d->n));
+    if (z)
+        CHECK(check_ld(d->ldz, d->n));
+    if (!d->m)
+        return DNNSEQ_OK;
+    if (any_null({x, w, y}) || (residual == y && d->ldresidual != d->ldy) || z == y)
+        return DNNSEQ_EINVAL;
+    if (bad_align({x, w, bias, residual, y, z, scratch}))
+        return DNNSEQ_EALIGN;
+    if (dsq::linear_forward_scratch(*d) && !scratch)
+        return DNNSEQ_ESCRATCH;
+    return status(dsq::launch_linear_forward(*d, x, w, bias, residual, y, z, scratch, (hipStream_t)hip_stream));
+}
+
+dnnseq_status dnnseq_linear_backward(const dnnseq_linear_desc *d, const void *x, const void *w, const void *z,
+                                     const void *dy, const void *dx_add, void *dx, void *dw, float *db,
+                                     void *scratch, void *hip_stream)
+{
+    CHECK(check_linear(d));
+    const bool needs_z = d->activation != DNNSEQ_ACT_NONE;
+    CHECK(check_ld(d->lddy, d->n));
+    if (needs_z)
+        CHECK(check_ld(d->ldz, d->n));
+    if (dx)
+        CHECK(check_ld(d->lddx, d->k));
+    if (dx && dx_add)
+        CHECK(check_ld(d->lddx_add, d->k));
+    if (dw)
+        CHECK(check_ld(d->lddw, d->k));
+    if (d->m && (any_null({dy}) || (dx && !w) || (dw && !x) || (needs_z && !z)))
+        return DNNSEQ_EINVAL;
+    if (dx && dx == dx_add && d->lddx != d->lddx_add)
+        return DNNSEQ_EINVAL;
+    if (bad_align({x, w, z, dy, dx_add, dx, dw, db, scratch}))
+        return DNNSEQ_EALIGN;
+    if (!dw && !db && !(dx && d->m))
+        return DNNSEQ_OK;
+    if (dsq::linear_backward_scratch(*d) && !scratch)
+        return DNNSEQ_ESCRATCH;
+    return status(
+        dsq::launch_linear_backward(*d, x, w, z, dy, dx_add, dx, dw, db, scratch, (hipStream_t)hip_stream));
+}
+
+size_t dnnseq_layernorm_backward_scratch_bytes(const dnnseq_layernorm_desc *d)
+{
+    // (the sizes alone decide: a descriptor made for the forward call gives the same)
+    return d && d->rows > 0 && d->cols > 0 && d->cols <= DNNSEQ_MAX_NORM_COLS ? dsq::norm_backward_scratch(*d) : 0;
+}
+
+dnnseq_status dnnseq_layernorm_forward(const dnnseq_layernorm_desc *d, const void *x, const float *gamma,
+                                       const float *beta, void *y, float *mean, float *rstd, void *hip_stream)
+{
+    CHECK(check_norm(d, false, false));
+    if (!d->rows)
+        return DNNSEQ_OK;
+    if (any_null({x, gamma, beta, y, mean, rstd}) || (x == y && d->ldx != d->ldy))
+        return DNNSEQ_EINVAL;
+    if (bad_align({x, gamma, beta, y, mean, rstd}))
+        return DNNSEQ_EALIGN;
+    return status(dsq::launch_norm_forward(*d, x, gamma, beta, y, mean, rstd, (hipStream_t)hip_stream));
+}
+
+dnnseq_status dnnseq_layernorm_backward(const dnnseq_layernorm_desc *d, const void *x, const void *dy,
+                                        const float *gamma, const float *mean, const float *rstd, const void *dx_add,
+                                        void *dx, float *dgamma, float *dbeta, void *scratch, void *hip_stream)
+{
+    CHECK(check_norm(d, true, dx_add != nullptr));
+    if (any_null({dgamma, dbeta}) || (d->rows && any_null({x, dy, gamma, mean, rstd, dx})) ||
+        (dx_add && dx == dx_add && d->lddx != d->lddx_add))
+        return DNNSEQ_EINVAL;
+    if (bad_align({x, dy, gamma, mean, rstd, dx_add, dx, dgamma, dbeta, scratch}))
+        return DNNSEQ_EALIGN;
+    if (d->rows && !scratch)
+        return DNNSEQ_ESCRATCH;
+    return status(dsq::launch_norm_backward(*d, x, dy, gamma, mean, rstd, dx_add, dx, dgamma, dbeta, scratch,
+                                            (hipStream_t)hip_stream));
+}
+
+} // extern "C"

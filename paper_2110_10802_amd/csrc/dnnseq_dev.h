@@ -1,0 +1,92 @@
+// Device-side helpers of the 16-bit sequence operators (attention, linear, layer normalisation).
+#pragma once
+#include "mbconv_dev.h"
+
+namespace dsq {
+
+using mbk::kWave;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+
+// The two storage types: conversions (round to nearest even, v_cvt_pk_*) and their matrix
+// instructions.  Operand fragments travel as eight 16-bit values in four registers.
+struct BF16 {
+    static constexpr bool kHalf = false;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return mbk::bf16_pack2(lo, hi); }
+    static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
+    static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+    static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+    static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c,
+                                                       0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c,
+                                                       0, 0, 0);
+    }
+};
+struct FP16 {
+    static constexpr bool kHalf = true;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi)
+    {
+        const f32x2 v = {lo, hi};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h16x2));
+    }
+    static __device__ __forceinline__ float one(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
+    static __device__ __forceinline__ float lo(uint32_t v) { return one((uint16_t)v); }
+    static __device__ __forceinline__ float hi(uint32_t v) { return one((uint16_t)(v >> 16)); }
+    static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c,
+                                                      0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h16x8, a), __builtin_bit_cast(h16x8, b), c,
+                                                      0, 0, 0);
+    }
+};
+template <class T>
+__device__ __forceinline__ uint16_t round16(float v)
+{
+    return (uint16_t)T::pack(v, v);
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes per lane from `base` + voff (bytes) straight into LDS, lane l of the wavefront to
+// dst + 16 l (dst the same in every lane).  Lanes at or past `bytes` write zeros: kNowhere sends a
+// lane there on purpose.
+constexpr uint32_t kNowhere = 0x7fffff00u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, void *dst, uint32_t voff)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)dst, 16, (int)voff, 0, 0, 0);
+}
+// Four 16-bit elements down a column: within 16 lanes, lane i names four elements of row i/4 at
+// columns 4 (i%4) and receives rows 0..3 of column i.
+__device__ __forceinline__ u32x2 read_tr(const uint16_t *p)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4 *)const_cast<uint16_t *>(p)));
+}
+__device__ __forceinline__ u32x4 join(u32x2 a, u32x2 b) { return u32x4{a[0], a[1], b[0], b[1]}; }
+
+__device__ __forceinline__ uint32_t wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+
+} // namespace dsq

@@ -1,0 +1,33 @@
+// Host-side launchers of the 16-bit sequence operators (internal to the library).
+#pragma once
+#include "../../include/dnnseq.h"
+#include <hip/hip_runtime.h>
+
+namespace dsq {
+
+hipError_t launch_linear_forward(const dnnseq_linear_desc &d, const void *x, const void *w, const float *bias,
+                                 const void *residual, void *y, void *z, void *scratch, hipStream_t st);
+size_t linear_forward_scratch(const dnnseq_linear_desc &d);
+hipError_t launch_linear_backward(const dnnseq_linear_desc &d, const void *x, const void *w, const void *z,
+                                  const void *dy, const void *dx_add, void *dx, void *dw, float *db, void *scratch,
+                                  hipStream_t st);
+size_t linear_backward_scratch(const dnnseq_linear_desc &d);
+
+hipError_t launch_norm_forward(const dnnseq_layernorm_desc &d, const void *x, const float *gamma, const float *beta,
+                               void *y, float *mean, float *rstd, hipStream_t st);
+hipError_t launch_norm_backward(const dnnseq_layernorm_desc &d, const void *x, const void *dy, const float *gamma,
+                                const float *mean, const float *rstd, const void *dx_add, void *dx, float *dgamma,
+                                float *dbeta, void *scratch, hipStream_t st);
+size_t norm_backward_scratch(const dnnseq_layernorm_desc &d);
+
+hipError_t launch_attention_forward(const dnnseq_attention_desc &d, const void *q, const void *k, const void *v,
+                                    const int32_t *q_lens, const int32_t *kv_lens, void *o, float *lse, void *scratch,
+                                    hipStream_t st);
+size_t attention_forward_scratch(const dnnseq_attention_desc &d);
+hipError_t launch_attention_backward(const dnnseq_attention_desc &d, const void *q, const void *k, const void *v,
+                                     const void *o, const void *dout, const float *lse, const int32_t *q_lens,
+                                     const int32_t *kv_lens, void *dq, void *dk, void *dv, void *scratch,
+                                     hipStream_t st);
+size_t attention_backward_scratch(const dnnseq_attention_desc &d);
+
+} // namespace dsq

@@ -1,0 +1,523 @@
+// Attention forward on 16-bit tensors: softmax(scale q k^T) v in one pass over the keys, with the
+// running maximum and sum of each row.
+//
+// The query heads of a key head are rows of one problem: row r of (request b, key head g) is token
+// r / group, head g group + r % group, so keys and values are read once for the group.  Scores are
+// computed transposed (keys as matrix rows, query rows as columns): a lane holds scores of one query
+// row only, the row's maximum takes one exchange between the halves of the wavefront, and the
+// probabilities are already where the second product, v^T p^T, wants them (dnnseq_attn.h).
+//
+//   attn_fwd    128 rows per workgroup, 32 per wavefront; keys and values in tiles of 64 through LDS,
+//               the next tile on its way while this one is multiplied
+//   attn_token  at most 16 rows (single tokens): bound by reading keys and values once; each wavefront
+//               walks its own chunks of 32 keys, keys from memory straight into operand order
+//   Either splits the keys over workgroups where there are few rows; attn_combine joins the parts.
+#include "dnnseq_attn.h"
+#include "dnnseq_launch.h"
+
+#include <algorithm>
+
+namespace dsq {
+namespace {
+
+struct Forward {
+    const uint16_t *q, *k, *v;
+    uint16_t *o;
+    float *lse; // may be null
+    const int32_t *q_lens, *kv_lens;
+    dnnseq_stride sq, sk, sv, so;
+    int batch, q_heads, kv_heads, group, q_len, kv_len, dim, causal;
+    float scale2; // scale * log2 e
+    int splits, per_split;   // keys per split, a multiple of 64
+    float *part_o, *part_lse; // [splits][batch][q_heads][q_len][dim], [splits][batch][q_heads][q_len]
+};
+
+// Where a row's results go.
+__device__ __forceinline__ size_t row_index(const Forward &a, int b, int g, int r)
+{
+    return ((size_t)b * a.q_heads + g * a.group + r % a.group) * a.q_len + r / a.group;
+}
+__device__ __forceinline__ int64_t row_offset(const dnnseq_stride &s, int b, int head, int token)
+{
+    return b * s.batch + head * s.head + token * s.token;
+}
+
+// One tile of 64 keys for 32 rows: `limit` is one past the last key the lane's row sees.
+template <class T, int NS, int RS, bool MASK>
+__device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const char *__restrict__ vt,
+                                             const AlongReader<RS> &along, const AcrossReader<RS> &across,
+                                             const u32x4 (&q)[2 * NS], f32x16 (&acc)[NS], float &m, float &l, int key0,
+                                             int limit, float scale2)
+{
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        s[b] = f32x16{};
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i)
+            s[b] = T::mma32(along.get(kt, b, i), q[i], s[b]);
+    }
+    if (MASK) {
+        const int j0 = key0 + (threadIdx.x % kWave) / 32 * 4;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[b][r] = j0 + 32 * b + 8 * (r / 4) + r % 4 < limit ? s[b][r] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            top = fmaxf(top, s[b][r]);
+    top = halves_max(top) * scale2;
+    // The reference point m follows the maximum only when that outgrows it by 2^8: p and the sums stay
+    // far inside fp32 and fp16, and most tiles leave the accumulators alone.
+    if (__any(top > m + 8.0f)) {
+        const float to = fmaxf(m, top), safe = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(m - safe);
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < NS; ++e)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[e][r] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], scale2, -ref));
+            l += s[b][r];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u32x4 p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) // rounded to the operands' type: p is at most 2^8, its error 2^-8 or 2^-11 of it
+                p[i] = T::pack(s[b][8 * h + 2 * i], s[b][8 * h + 2 * i + 1]);
+#pragma unroll
+            for (int e = 0; e < NS; ++e)
+                acc[e] = T::mma32(across.get(vt, 2 * b + h, e), p, acc[e]);
+        }
+    }
+}
+
+template <class T, int NS>
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Forward a)
+{
+    constexpr int RS = NS > 2 ? 128 : 64, ROWS = 128;
+    typedef TileLoader<RS, 256> Load;
+    __shared__ __attribute__((aligned(256))) char lds[4 * Load::kBytes]; // [2][keys, values]
+    const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
+    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
+    const int unit = item / tiles, b = unit / a.kv_heads, g = unit % a.kv_heads;
+    const int r0 = (tiles - 1 - item % tiles) * ROWS; // the rows that see most keys first
+    const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
+    const int lane = threadIdx.x % kWave, w = wave_id();
+    const int first = blockIdx.y * a.per_split, last = min(kl, first + a.per_split);
+    // one past the last key that a row sees
+    const auto limit_of = [&](int r) {
+        const int t = r / a.group;
+        return r >= rows || t >= ql ? 0 : a.causal ? min(last, t + kl - ql + 1) : last;
+    };
+    const int r = r0 + w * 32 + lane % 32, limit = limit_of(r);
+    // of the whole workgroup (the limits grow along the rows up to the last valid one), of the
+    // wavefront, and the smallest of the wavefront's valid rows
+    const int end = limit_of(min(r0 + ROWS, ql * a.group) - 1 >= r0 ? min(r0 + ROWS, ql * a.group) - 1 : rows);
+    const int wr = min(r0 + w * 32 + 32, ql * a.group) - 1;
+    const int wave_end = wr >= r0 + w * 32 ? limit_of(wr) : 0;
+    // without masking: all 32 rows see the whole tile
+    const int wave_free = min(limit_of(r0 + w * 32), limit_of(r0 + w * 32 + 31));
+
+    u32x4 q[2 * NS];
+    const int head = g * a.group + r % a.group, token = r / a.group;
+    const uint16_t *qrow = a.q + row_offset(a.sq, b, head, token);
+#pragma unroll
+    for (int i = 0; i < 2 * NS; ++i)
+        q[i] = own_fragment(qrow, r < rows && token < ql, a.dim, i);
+    Load lk, lv;
+    lk.init(a.k + row_offset(a.sk, b, g, 0), a.sk.token, a.dim);
+    lv.init(a.v + row_offset(a.sv, b, g, 0), a.sv.token, a.dim);
+    AlongReader<RS> along;
+    AcrossReader<RS> across;
+    along.init();
+    across.init();
+    f32x16 acc[NS];
+#pragma unroll
+    for (int e = 0; e < NS; ++e)
+        acc[e] = f32x16{};
+    float m = -INFINITY, l = 0.f;
+    if (first < end) {
+        lk.load(lds, first, kl);
+        lv.load(lds + Load::kBytes, first, kl);
+    }
+    for (int k0 = first, turn = 0; k0 < end; k0 += kTileRows, turn ^= 1) {
+        char *cur = lds + turn * (2 * Load::kBytes), *nxt = lds + (turn ^ 1) * (2 * Load::kBytes);
+        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
+        __syncthreads();                    // and everyone's; the other buffer is no longer read
+        const auto step = [&](const char *__restrict__ c, char *__restrict__ n) __attribute__((always_inline)) {
+            if (k0 + kTileRows < end) {
+                lk.load(n, k0 + kTileRows, kl);
+                lv.load(n + Load::kBytes, k0 + kTileRows, kl);
+            }
+            if (k0 + kTileRows <= wave_free)
+                forward_tile<T, NS, RS, false>(c, c + Load::kBytes, along, across, q, acc, m, l, k0, limit, a.scale2);
+            else if (k0 < wave_end)
+                forward_tile<T, NS, RS, true>(c, c + Load::kBytes, along, across, q, acc, m, l, k0, limit, a.scale2);
+        };
+        step(cur, nxt);
+    }
+    l = halves_sum(l);
+    if (r >= rows)
+        return;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float lse = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+    const size_t ri = row_index(a, b, g, r);
+    if (a.part_o) {
+        const size_t all = (size_t)a.batch * a.q_heads * a.q_len, at = blockIdx.y * all + ri;
+        if (lane < 32)
+            a.part_lse[at] = lse;
+        if (lse == -INFINITY)
+            return;
+#pragma unroll
+        for (int e = 0; e < NS; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = 32 * e + 8 * i + lane / 32 * 4;
+                if (d < a.dim)
+                    *(f32x4 *)(a.part_o + at * a.dim + d) = f32x4{acc[e][4 * i] * inv, acc[e][4 * i + 1] * inv,
+                                                                  acc[e][4 * i + 2] * inv, acc[e][4 * i + 3] * inv};
+            }
+        return;
+    }
+    if (a.lse && lane < 32)
+        a.lse[ri] = lse;
+    uint16_t *orow = a.o + row_offset(a.so, b, head, token);
+#pragma unroll
+    for (int e = 0; e < NS; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 32 * e + 8 * i + lane / 32 * 4;
+            if (d < a.dim)
+                *(u32x2 *)(orow + d) = u32x2{T::pack(acc[e][4 * i] * inv, acc[e][4 * i + 1] * inv),
+                                             T::pack(acc[e][4 * i + 2] * inv, acc[e][4 * i + 3] * inv)};
+        }
+}
+
+// ---- at most 16 rows -----------------------------------------------------------------------------
+// Products of 16x16x32: scores of 16 keys x 16 rows, two of them giving the 32 keys that the second
+// product contracts (lane l holds keys 4 (l/16) + r of both; the transposing reads of the values use
+// the same order).
+constexpr int kChunk = 32;
+
+template <int RS>
+__device__ __forceinline__ int chunk_swizzle(int row)
+{
+    return (RS == 128 ? row & 7 : row >> 1 & 3) << 1;
+}
+
+template <class T, int NS>
+__global__ __launch_bounds__(256) void attn_token_kernel(Forward a)
+{
+    constexpr int RS = NS > 2 ? 128 : 64, UNITS = RS / 8, VLOADS = kChunk * UNITS / kWave;
+    constexpr int VBYTES = kChunk * RS * 2;
+    __shared__ __attribute__((aligned(256))) char lds[4 * 2 * VBYTES]; // [4 wavefronts][2][32 values]
+    __shared__ float wm[4][16], wl[4][16];
+    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
+    const int split = item % a.splits, unit = item / a.splits, b = unit / a.kv_heads, g = unit % a.kv_heads;
+    const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
+    const int rows = a.q_len * a.group, lane = threadIdx.x % kWave, w = wave_id();
+    const int first = split * a.per_split, last = min(kl, first + a.per_split);
+    const int r = lane % 16, token = r / a.group, head = g * a.group + r % a.group;
+    const bool live = r < rows && token < ql;
+    const int limit = live ? (a.causal ? min(last, token + kl - ql + 1) : last) : 0;
+    const int end = ql > 0 ? last : 0; // (the last token sees every key)
+
+    u32x4 q[NS];
+    const uint16_t *qrow = a.q + row_offset(a.sq, b, head, token);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int c = 32 * s + lane / 16 * 8;
+        q[s] = live && c < a.dim ? *(const u32x4 *)(qrow + c) : u32x4{0, 0, 0, 0};
+    }
+    const uint32_t kpitch = (uint32_t)a.sk.token * 2, vpitch = (uint32_t)a.sv.token * 2, width = a.dim * 2;
+    const char *kbase = (const char *)(a.k + row_offset(a.sk, b, g, 0));
+    const char *vbase = (const char *)(a.v + row_offset(a.sv, b, g, 0));
+    uint32_t koff[NS], voff[VLOADS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int c = 32 * s + lane / 16 * 8;
+        koff[s] = c < a.dim ? (lane % 16) * kpitch + c * 2 : kNowhere;
+    }
+#pragma unroll
+    for (int i = 0; i < VLOADS; ++i) {
+        const int id = i * kWave + lane, row = id / UNITS, unit8 = id % UNITS ^ chunk_swizzle<RS>(row);
+        voff[i] = unit8 * 8 < a.dim ? row * vpitch + unit8 * 16 : kNowhere;
+    }
+    // transposing reads: lane i of a group of 16 names row 4 g + i/4, elements 4 (i % 4) of a block of 16
+    const int ti = lane % 16, trow = lane / 16 * 4 + ti / 4;
+    const uint32_t tbase = trow * (RS * 2) + ti % 2 * 8, tflip = (ti % 4 / 2 ^ chunk_swizzle<RS>(trow)) * 16;
+
+    u32x4 kf[2][2][NS]; // [buffer][16 keys][32 elements]
+    char *mine = lds + w * (2 * VBYTES);
+    const auto fetch = [&](int key0, u32x4(&kr)[2][NS], char *vl) __attribute__((always_inline)) {
+        const int n = min(kl - key0, kChunk);
+        const auto rk = buffer(kbase + (int64_t)key0 * kpitch, (n - 1) * kpitch + width);
+        const auto rv = buffer(vbase + (int64_t)key0 * vpitch, (n - 1) * vpitch + width);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                kr[h][s] = __builtin_bit_cast(
+                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                               rk, koff[s] == kNowhere ? (int)kNowhere : (int)(koff[s] + h * 16 * kpitch), 0, 0));
+#pragma unroll
+        for (int i = 0; i < VLOADS; ++i)
+            load_lds(rv, vl + i * (kWave * 16), voff[i]);
+    };
+    f32x4 acc[2 * NS];
+#pragma unroll
+    for (int e = 0; e < 2 * NS; ++e)
+        acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    const auto chunk = [&](int key0, const u32x4(&kr)[2][NS], const char *__restrict__ vl) __attribute__((always_inline)) {
+        f32x4 s[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                s[h] = T::mma16(kr[h][i], q[i], s[h]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[h][i] = key0 + 16 * h + lane / 16 * 4 + i < limit ? s[h][i] : -INFINITY;
+                top = fmaxf(top, s[h][i]);
+            }
+        }
+        top = quarters_max(top) * a.scale2;
+        if (__any(top > m + 8.0f)) {
+            const float to = fmaxf(m, top), safe = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(m - safe);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < 2 * NS; ++e)
+                acc[e] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        u32x4 p;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[h][i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], a.scale2, -ref));
+                l += s[h][i];
+            }
+            p[2 * h] = T::pack(s[h][0], s[h][1]);
+            p[2 * h + 1] = T::pack(s[h][2], s[h][3]);
+        }
+#pragma unroll
+        for (int e = 0; e < 2 * NS; ++e) {
+            const char *v = vl + tbase + (tflip ^ (e * 32));
+            acc[e] = T::mma16(join(read_tr((const uint16_t *)v), read_tr((const uint16_t *)(v + 16 * RS * 2))), p,
+                              acc[e]);
+        }
+    };
+
+    const auto landed = [] {
+        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0)
+        asm volatile("" ::: "memory");      // no read of LDS moves above it
+    };
+    // chunks w, w + 4, ...: everything that was requested has landed, the next is requested, this one used
+    int k0 = first + w * kChunk;
+    if (k0 < end)
+        fetch(k0, kf[0], mine);
+    for (; k0 < end; k0 += 8 * kChunk) {
+        const int k1 = k0 + 4 * kChunk, k2 = k0 + 8 * kChunk;
+        landed();
+        if (k1 < end)
+            fetch(k1, kf[1], mine + VBYTES);
+        chunk(k0, kf[0], mine);
+        if (k1 >= end)
+            break;
+        landed();
+        if (k2 < end)
+            fetch(k2, kf[0], mine);
+        chunk(k1, kf[1], mine + VBYTES);
+    }
+    l = quarters_sum(l);
+    __syncthreads(); // the values' buffers become the wavefronts' results: [4][16 rows][RS]
+    float *out = (float *)lds;
+    if (lane < 16) {
+        wm[w][lane] = m;
+        wl[w][lane] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < 2 * NS; ++e)
+        *(f32x4 *)(out + (w * 16 + r) * RS + 16 * e + lane / 16 * 4) = acc[e];
+    __syncthreads();
+    // 16 threads to a row, 8 elements each
+    const int row = threadIdx.x / 16, c = threadIdx.x % 16 * 8;
+    if (row >= rows)
+        return;
+    float top = -INFINITY, total = 0.f, f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        top = fmaxf(top, wm[i][row]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = __builtin_amdgcn_exp2f(wm[i][row] - ref);
+        total += f[i] * wl[i][row];
+    }
+    const float inv = total == 0.f ? 0.f : 1.0f / total;
+    const float lse = total == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(total)) * kLn2;
+    const size_t ri = row_index(a, b, g, row);
+    float v[8];
+    if (c < a.dim)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s += f[j] * out[(j * 16 + row) * RS + c + i];
+            v[i] = s * inv;
+        }
+    if (a.part_o) {
+        const size_t at = (size_t)split * a.batch * a.q_heads * a.q_len + ri;
+        if (c == 0)
+            a.part_lse[at] = lse;
+        if (c < a.dim && lse != -INFINITY) {
+            *(f32x4 *)(a.part_o + at * a.dim + c) = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4 *)(a.part_o + at * a.dim + c + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+        return;
+    }
+    if (a.lse && c == 0)
+        a.lse[ri] = lse;
+    if (c < a.dim)
+        *(u32x4 *)(a.o + row_offset(a.so, b, g * a.group + row % a.group, row / a.group) + c) =
+            u32x4{T::pack(v[0], v[1]), T::pack(v[2], v[3]), T::pack(v[4], v[5]), T::pack(v[6], v[7])};
+}
+
+// The parts of a row joined: weights exp(lse_s - lse).  A wavefront per row, two elements per lane.
+template <class T>
+__global__ __launch_bounds__(256) void attn_combine_kernel(Forward a)
+{
+    const size_t all = (size_t)a.batch * a.q_heads * a.q_len;
+    const size_t ri = blockIdx.x * (size_t)4 + wave_id();
+    if (ri >= all)
+        return;
+    const int lane = threadIdx.x % kWave, c = lane * 2;
+    float top = -INFINITY;
+    for (int s = 0; s < a.splits; ++s)
+        top = fmaxf(top, a.part_lse[s * all + ri]);
+    float total = 0.f, x = 0.f, y = 0.f;
+    if (top != -INFINITY)
+        for (int s = 0; s < a.splits; ++s) {
+            const float e = a.part_lse[s * all + ri];
+            if (e == -INFINITY)
+                continue;
+            const float f = __builtin_amdgcn_exp2f((e - top) * kLog2e);
+            total += f;
+            if (c < a.dim) {
+                const f32x2 v = *(const f32x2 *)(a.part_o + (s * all + ri) * a.dim + c);
+                x = fmaf(f, v[0], x);
+                y = fmaf(f, v[1], y);
+            }
+        }
+    const float inv = total == 0.f ? 0.f : 1.0f / total;
+    const int token = ri % a.q_len, head = ri / a.q_len % a.q_heads, b = ri / a.q_len / a.q_heads;
+    if (a.lse && lane == 0)
+        a.lse[ri] = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
+    if (c < a.dim)
+        *(uint32_t *)(a.o + row_offset(a.so, b, head, token) + c) = T::pack(x * inv, y * inv);
+}
+
+struct Plan {
+    bool token;
+    int items, splits, per_split;
+};
+Plan plan(const dnnseq_attention_desc &d)
+{
+    Plan p;
+    const int64_t rows = (int64_t)d.q_len * (d.q_heads / d.kv_heads);
+    p.token = rows <= 16;
+    const int64_t items = (int64_t)d.batch * d.kv_heads * (p.token ? 1 : (rows + 127) / 128);
+    p.items = (int)items;
+    // keys per workgroup: enough workgroups to fill the 256 CUs, but no shorter than what hides a
+    // workgroup's start and the joining
+    const int64_t want = std::max<int64_t>(1, (p.token ? 2048 : 512) / std::max<int64_t>(items, 1));
+    const int64_t least = 512;
+    const int64_t per = std::max(least, ((d.kv_len + want - 1) / want + 63) / 64 * 64);
+    p.per_split = (int)per;
+    p.splits = (int)std::max<int64_t>(1, (d.kv_len + per - 1) / per);
+    if (p.splits == 1)
+        p.per_split = (std::max(d.kv_len, 1) + 63) / 64 * 64;
+    return p;
+}
+
+template <class T, int NS>
+hipError_t forward(Forward a, const Plan &p, hipStream_t st)
+{
+    if (p.token)
+        attn_token_kernel<T, NS><<<p.items * p.splits, 256, 0, st>>>(a);
+    else
+        attn_fwd_kernel<T, NS><<<dim3(p.items, p.splits), 256, 0, st>>>(a);
+    if (p.splits > 1) {
+        const size_t rows = (size_t)a.batch * a.q_heads * a.q_len;
+        attn_combine_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t forward_dim(const Forward &a, const Plan &p, hipStream_t st)
+{
+    switch ((a.dim + 31) / 32) {
+    case 1:
+        return forward<T, 1>(a, p, st);
+    case 2:
+        return forward<T, 2>(a, p, st);
+    case 3:
+        return forward<T, 3>(a, p, st);
+    default:
+        return forward<T, 4>(a, p, st);
+    }
+}
+
+} // namespace
+
+size_t attention_forward_scratch(const dnnseq_attention_desc &d)
+{
+    if (!d.batch || !d.q_len)
+        return 0;
+    const Plan p = plan(d);
+    return p.splits > 1 ? (size_t)p.splits * d.batch * d.q_heads * d.q_len * (d.head_dim + 1) * 4 : 0;
+}
+
+hipError_t launch_attention_forward(const dnnseq_attention_desc &d, const void *q, const void *k, const void *v,
+                                    const int32_t *q_lens, const int32_t *kv_lens, void *o, float *lse, void *scratch,
+                                    hipStream_t st)
+{
+    const Plan p = plan(d);
+    Forward a = {};
+    a.q = (const uint16_t *)q, a.k = (const uint16_t *)k, a.v = (const uint16_t *)v, a.o = (uint16_t *)o;
+    a.lse = lse, a.q_lens = q_lens, a.kv_lens = kv_lens;
+    a.sq = d.q, a.sk = d.k, a.sv = d.v, a.so = d.o;
+    a.batch = d.batch, a.q_heads = d.q_heads, a.kv_heads = d.kv_heads, a.group = d.q_heads / d.kv_heads;
+    a.q_len = d.q_len, a.kv_len = d.kv_len, a.dim = d.head_dim, a.causal = d.causal;
+    a.scale2 = d.scale * kLog2e;
+    a.splits = p.splits, a.per_split = p.per_split;
+    if (p.splits > 1) {
+        a.part_o = (float *)scratch;
+        a.part_lse = a.part_o + (size_t)p.splits * d.batch * d.q_heads * d.q_len * d.head_dim;
+    }
+    return d.dtype == DNNSEQ_FP16 ? forward_dim<FP16>(a, p, st) : forward_dim<BF16>(a, p, st);
+}
+
+} // namespace dsq

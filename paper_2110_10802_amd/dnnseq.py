@@ -1,0 +1,218 @@
+"""ctypes binding of the 16-bit sequence operators of libmbconv.so: attention, linear layers and
+layer normalisation (argument marshalling only; mirrors include/dnnseq.h).  Tensors are anything
+with a ``data_ptr()`` method; the ``*_desc`` functions also read ``shape``, ``stride()`` and
+``dtype`` (torch tensors on any device, views included).  A descriptor depends on sizes, types and
+strides alone: make it once and keep it.  There is no fallback: if the HIP library is missing,
+loading raises."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Any, Optional
+
+from . import binding as _B
+
+EXPORTS = ["dnnseq_attention_forward_scratch_bytes", "dnnseq_attention_backward_scratch_bytes",
+           "dnnseq_attention_forward", "dnnseq_attention_backward", "dnnseq_linear_forward_scratch_bytes",
+           "dnnseq_linear_backward_scratch_bytes", "dnnseq_linear_forward", "dnnseq_linear_backward",
+           "dnnseq_layernorm_backward_scratch_bytes", "dnnseq_layernorm_forward", "dnnseq_layernorm_backward"]
+MAX_HEAD_DIM = 128
+MAX_NORM_COLS = 16384
+DTYPES = {"bfloat16": 0, "float16": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "mish": 4}
+_lib = None
+
+
+class DnnSeqError(RuntimeError):
+    def __init__(self, status: int, where: str):
+        super().__init__(f"{where}: status {status}")
+        self.status = status
+
+
+class Stride(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "q_heads", "kv_heads", "q_len", "kv_len", "head_dim",
+                                         "causal")] + \
+               [("scale", C.c_float)] + [(n, Stride) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "activation", "m", "n", "k", "dw_fp32")] + \
+               [(n, C.c_int64) for n in ("ldx", "ldw", "ldy", "ldresidual", "ldz", "lddy", "lddx", "lddx_add",
+                                         "lddw")]
+
+
+class LayerNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "cols")] + [("eps", C.c_float)] + \
+               [(n, C.c_int64) for n in ("ldx", "ldy", "lddy", "lddx", "lddx_add")]
+
+
+def load():
+    global _lib
+    if _lib is None:
+        lib = _B.load()
+        vp, at, li, ln = C.c_void_p, C.POINTER(AttentionDesc), C.POINTER(LinearDesc), C.POINTER(LayerNormDesc)
+        lib.dnnseq_attention_forward_scratch_bytes.argtypes = [at]
+        lib.dnnseq_attention_backward_scratch_bytes.argtypes = [at]
+        lib.dnnseq_attention_forward.argtypes = [at] + [vp] * 9
+        lib.dnnseq_attention_backward.argtypes = [at] + [vp] * 13
+        lib.dnnseq_linear_forward_scratch_bytes.argtypes = [li]
+        lib.dnnseq_linear_backward_scratch_bytes.argtypes = [li]
+        lib.dnnseq_linear_forward.argtypes = [li] + [vp] * 8
+        lib.dnnseq_linear_backward.argtypes = [li] + [vp] * 10
+        lib.dnnseq_layernorm_backward_scratch_bytes.argtypes = [ln]
+        lib.dnnseq_layernorm_forward.argtypes = [ln] + [vp] * 7
+        lib.dnnseq_layernorm_backward.argtypes = [ln] + [vp] * 11
+        for n in EXPORTS:
+            getattr(lib, n).restype = C.c_size_t if n.endswith("scratch_bytes") else C.c_int
+        _lib = lib
+    return _lib
+
+
+def _ptr(t: Any):
+    if t is None or isinstance(t, int):
+        return t
+    return t.data_ptr()
+
+
+def _check(rc: int, where: str):
+    if rc != 0:
+        raise DnnSeqError(rc, where)
+
+
+def _dtype(t) -> int:
+    name = str(t.dtype).rsplit(".", 1)[-1]
+    if name not in DTYPES:
+        raise ValueError(f"dnnseq: tensors are bfloat16 or float16, not {name}")
+    return DTYPES[name]
+
+
+def _same_dtype(first, *others) -> int:
+    dt = _dtype(first)
+    if any(t is not None and _dtype(t) != dt for t in others):
+        raise ValueError("dnnseq: the tensors of a call have one type")
+    return dt
+
+
+# ---- attention --------------------------------------------------------------------------------
+
+def attention_desc(q, k, v, o, causal: bool = False, scale: Optional[float] = None, dout=None, dq=None, dk=None,
+                   dv=None) -> AttentionDesc:
+    """Descriptor of a call on tensors (views) [batch, heads, length, dim].  ``scale``: 1/sqrt(dim)
+    unless given.  ``dout``, ``dq``, ``dk``, ``dv``: for backward; the strides of o, q, k and v
+    where they are not given."""
+    dt = _same_dtype(q, k, v, o, dout, dq, dk, dv)
+    B, H, Q, D = q.shape
+    G, K = k.shape[1], k.shape[2]
+    for t, s in ((k, (B, G, K, D)), (v, (B, G, K, D)), (o, (B, H, Q, D)), (dout, (B, H, Q, D)), (dq, (B, H, Q, D)),
+                 (dk, (B, G, K, D)), (dv, (B, G, K, D))):
+        if t is not None and (tuple(t.shape) != s or (s[3] > 1 and t.stride(3) != 1)):
+            raise ValueError("dnnseq: attention takes [batch, heads, length, dim] with a contiguous dim")
+    if (q.stride(3) != 1 and D > 1) or (0 < D and q.dim() != 4):
+        raise ValueError("dnnseq: attention takes [batch, heads, length, dim] with a contiguous dim")
+
+    def st(t, like):
+        t = like if t is None else t
+        # (torch gives dimensions of one element any stride: what is never stepped over is 0)
+        return Stride(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+
+    return AttentionDesc(dt, B, H, G, Q, K, D, int(causal), D ** -0.5 if scale is None else scale, st(q, q), st(k, k),
+                         st(v, v), st(o, o), st(dout, o), st(dq, q), st(dk, k), st(dv, v))
+
+
+def attention_forward_scratch_bytes(desc: AttentionDesc) -> int:
+    return load().dnnseq_attention_forward_scratch_bytes(desc)
+
+
+def attention_backward_scratch_bytes(desc: AttentionDesc) -> int:
+    return load().dnnseq_attention_backward_scratch_bytes(desc)
+
+
+def attention_forward(desc: AttentionDesc, q, k, v, o, lse=None, q_lens=None, kv_lens=None, scratch=None,
+                      stream: int = 0) -> None:
+    _check(load().dnnseq_attention_forward(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(q_lens), _ptr(kv_lens), _ptr(o),
+                                           _ptr(lse), _ptr(scratch), stream or None), "dnnseq_attention_forward")
+
+
+def attention_backward(desc: AttentionDesc, q, k, v, o, dout, lse, dq, dk, dv, scratch, q_lens=None, kv_lens=None,
+                       stream: int = 0) -> None:
+    _check(load().dnnseq_attention_backward(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse),
+                                            _ptr(q_lens), _ptr(kv_lens), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(scratch),
+                                            stream or None), "dnnseq_attention_backward")
+
+
+# ---- linear -----------------------------------------------------------------------------------
+
+def linear_desc(x, w, activation: str = "none", y=None, residual=None, z=None, dy=None, dx=None, dx_add=None,
+                dw=None) -> LinearDesc:
+    """Descriptor of a call on matrices x [m, k] and w [n, k] (views with contiguous rows).  Matrices
+    that are not given are taken to be contiguous."""
+    dt = _same_dtype(x, w, y, residual, z, dy, dx, dx_add)
+    (m, k), n = x.shape, w.shape[0]
+    fp32 = dw is not None and str(dw.dtype).endswith("float32")
+    if dw is not None and not fp32:
+        _same_dtype(x, dw)
+
+    def ld(t, rows, cols):
+        if t is None:
+            return cols
+        if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+            raise ValueError("dnnseq: linear takes x [m, k], w [n, k], y [m, n] with contiguous rows")
+        return t.stride(0) if rows > 1 else cols
+
+    return LinearDesc(dt, ACTIVATIONS[activation], m, n, k, int(fp32), ld(x, m, k), ld(w, n, k), ld(y, m, n),
+                      ld(residual, m, n), ld(z, m, n), ld(dy, m, n), ld(dx, m, k), ld(dx_add, m, k), ld(dw, n, k))
+
+
+def linear_forward_scratch_bytes(desc: LinearDesc) -> int:
+    return load().dnnseq_linear_forward_scratch_bytes(desc)
+
+
+def linear_backward_scratch_bytes(desc: LinearDesc) -> int:
+    return load().dnnseq_linear_backward_scratch_bytes(desc)
+
+
+def linear_forward(desc: LinearDesc, x, w, y, bias=None, residual=None, z=None, scratch=None, stream: int = 0) -> None:
+    _check(load().dnnseq_linear_forward(desc, _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(z),
+                                        _ptr(scratch), stream or None), "dnnseq_linear_forward")
+
+
+def linear_backward(desc: LinearDesc, x, w, dy, z=None, dx=None, dx_add=None, dw=None, db=None, scratch=None,
+                    stream: int = 0) -> None:
+    _check(load().dnnseq_linear_backward(desc, _ptr(x), _ptr(w), _ptr(z), _ptr(dy), _ptr(dx_add), _ptr(dx), _ptr(dw),
+                                         _ptr(db), _ptr(scratch), stream or None), "dnnseq_linear_backward")
+
+
+# ---- layer normalisation ----------------------------------------------------------------------
+
+def layernorm_desc(x, eps: float = 1e-5, y=None, dy=None, dx=None, dx_add=None) -> LayerNormDesc:
+    """Descriptor of a call on rows x [rows, cols] (views with contiguous rows).  Matrices that are
+    not given are taken to be contiguous."""
+    rows, cols = x.shape
+
+    def ld(t):
+        if t is None:
+            return cols
+        if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+            raise ValueError("dnnseq: layernorm takes [rows, cols] with contiguous rows")
+        return t.stride(0) if rows > 1 else cols
+
+    return LayerNormDesc(_same_dtype(x, y, dy, dx, dx_add), rows, cols, eps, ld(x), ld(y), ld(dy), ld(dx), ld(dx_add))
+
+
+def layernorm_backward_scratch_bytes(desc: LayerNormDesc) -> int:
+    return load().dnnseq_layernorm_backward_scratch_bytes(desc)
+
+
+def layernorm_forward(desc: LayerNormDesc, x, gamma, beta, y, mean, rstd, stream: int = 0) -> None:
+    _check(load().dnnseq_layernorm_forward(desc, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                           stream or None), "dnnseq_layernorm_forward")
+
+
+def layernorm_backward(desc: LayerNormDesc, x, dy, gamma, mean, rstd, dx, dgamma, dbeta, scratch, dx_add=None,
+                       stream: int = 0) -> None:
+    _check(load().dnnseq_layernorm_backward(desc, _ptr(x), _ptr(dy), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                            _ptr(dx_add), _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(scratch),
+                                            stream or None), "dnnseq_layernorm_backward")

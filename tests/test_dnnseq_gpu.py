@@ -1,0 +1,471 @@
+"""Attention, linear layers and layer normalisation on 16-bit tensors (through the C ABI) against
+64-bit references, with the tolerances that dnnseq_ref derives for every element."""
+import math
+
+import pytest
+import torch
+
+import dnnseq_ref as ref
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+NAN = float("nan")
+
+
+def _S():
+    from paper_2110_10802_amd import dnnseq
+    return dnnseq
+
+
+def _gen(*key):
+    seed = 1
+    for k in key:
+        seed = (seed * 1000003 + hash(int(k))) % (2 ** 31)
+    return torch.Generator().manual_seed(seed)
+
+
+def _scratch(nbytes):
+    """Scratch filled with NaN: nothing may be read from it that the call has not written."""
+    return torch.full((max(nbytes, 16) // 4 + 4,), NAN, device="cuda:0")
+
+
+def _placed(t, order="bhtd", pad=0, dtype=None):
+    """t [batch, heads, length, dim] on the GPU, its dimensions in memory in the given order and each
+    row (token) followed by `pad` elements of NaN."""
+    perm = ["bhtd".index(c) for c in order]
+    base = torch.full(tuple(t.shape[i] for i in perm[:3]) + (t.shape[3] + pad,), NAN, dtype=dtype or t.dtype,
+                      device="cuda:0")
+    base[..., :t.shape[3]] = t.permute(*perm).to(base)
+    inv = [order.index(c) for c in "bhtd"]
+    return base.permute(*inv)[..., :t.shape[3]]
+
+
+def _attention(dt, B, H, G, Q, K, D, causal=False, q_lens=None, kv_lens=None, orders=("bthd", "bthd"), pad=0,
+               scale=None, std=1.5, backward=True, garbage=NAN, repeat=False):
+    S = _S()
+    gen = _gen(B, H, G, Q, K, D, causal)
+    q = (torch.randn(B, H, Q, D, generator=gen) * std).to(dt)
+    k = torch.randn(B, G, K, D, generator=gen).to(dt)
+    v = torch.randn(B, G, K, D, generator=gen).to(dt)
+    do = torch.randn(B, H, Q, D, generator=gen).to(dt)
+    scale = D ** -0.5 if scale is None else scale
+    want, tol = ref.attention(q, k, v, scale, causal, q_lens, kv_lens, do if backward else None)
+    for b in range(B):  # what lies past a request's lengths may be anything
+        if q_lens is not None:
+            q[b, :, q_lens[b]:], do[b, :, q_lens[b]:] = garbage, garbage
+        if kv_lens is not None:
+            k[b, :, kv_lens[b]:], v[b, :, kv_lens[b]:] = garbage, garbage
+    qd, kd, vd = _placed(q, orders[0], pad), _placed(k, orders[1], pad), _placed(v, orders[1], pad)
+    od = _placed(torch.full_like(q, NAN), orders[0], pad)
+    ql = None if q_lens is None else torch.tensor(q_lens, dtype=torch.int32, device="cuda:0")
+    kl = None if kv_lens is None else torch.tensor(kv_lens, dtype=torch.int32, device="cuda:0")
+    lse = torch.full((B, H, Q), NAN, device="cuda:0")
+    print(f"[dnnseq] attention {dt} B{B} H{H}/{G} Q{Q} K{K} D{D} causal={causal} {q_lens} {kv_lens}", flush=True)
+    dod = _placed(do, orders[0], pad)
+    grads = {"dq": _placed(torch.full_like(q, NAN), orders[0], pad),
+             "dk": _placed(torch.full_like(k, NAN), orders[1], pad),
+             "dv": _placed(torch.full_like(v, NAN), orders[1], pad)}
+    desc = S.attention_desc(qd, kd, vd, od, causal=causal, scale=scale, dout=dod, **grads)
+    ws = _scratch(S.attention_forward_scratch_bytes(desc))
+    S.attention_forward(desc, qd, kd, vd, od, lse=lse, q_lens=ql, kv_lens=kl, scratch=ws)
+    torch.cuda.synchronize()
+    ref.check("o", od, want["o"], tol["o"])
+    ref.check("lse", lse, want["lse"], tol["lse"])
+    if not backward:
+        return
+    ws = _scratch(S.attention_backward_scratch_bytes(desc))
+    S.attention_backward(desc, qd, kd, vd, od, dod, lse, grads["dq"], grads["dk"], grads["dv"], ws, q_lens=ql,
+                         kv_lens=kl)
+    torch.cuda.synchronize()
+    for n in ("dv", "dk", "dq"):
+        ref.check(n, grads[n], want[n], tol[n])
+    if repeat:
+        first = [od.clone(), lse.clone()] + [grads[n].clone() for n in ("dq", "dk", "dv")]
+        S.attention_forward(desc, qd, kd, vd, od, lse=lse, q_lens=ql, kv_lens=kl,
+                            scratch=_scratch(S.attention_forward_scratch_bytes(desc)))
+        S.attention_backward(desc, qd, kd, vd, od, dod, lse, grads["dq"], grads["dk"], grads["dv"], ws, q_lens=ql,
+                             kv_lens=kl)
+        torch.cuda.synchronize()
+        for a, b in zip(first, [od, lse, grads["dq"], grads["dk"], grads["dv"]]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [8, 24, 32, 40, 64, 72, 80, 96, 104, 128])
+def test_attention_head_dims(dtype, dim):
+    _attention(TYPES[dtype], 2, 4, 2, 70, 131, dim, causal=dim % 16 == 0, pad=8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Q,K", [(1, 1), (1, 2), (2, 1), (31, 33), (64, 64), (65, 63), (128, 128), (129, 257), (300, 40)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_lengths(dtype, Q, K, causal):
+    _attention(TYPES[dtype], 1, 2, 2, Q, K, 64, causal=causal)
+
+
+@pytest.mark.parametrize("Q,K", [(0, 5), (5, 0), (1, 0), (90, 0)])
+def test_attention_lengths_of_zero(Q, K):
+    S = _S()
+    q, k = (torch.randn(2, 2, n, 64).to(torch.bfloat16).cuda() for n in (Q, K))
+    o, dq, dk, dv = (torch.full_like(t, NAN) for t in (q, q, k, k))
+    lse = torch.full((2, 2, Q), NAN, device="cuda:0")
+    d = S.attention_desc(q, k, k, o, causal=True)
+    ws = _scratch(max(S.attention_forward_scratch_bytes(d), S.attention_backward_scratch_bytes(d)))
+    S.attention_forward(d, q, k, k, o, lse=lse, scratch=ws)
+    S.attention_backward(d, q, k, k, o, q, lse, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    assert all((t == 0).all() for t in (o, dq, dk, dv)) and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 1), (8, 2), (7, 7), (14, 2), (20, 1)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_shared_heads(H, G, dim):
+    _attention(torch.bfloat16, 2, H, G, 75, 90, dim, causal=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("garbage", [NAN, math.inf, -math.inf])
+def test_attention_ragged_batches_and_what_lies_past_them(dtype, causal, garbage):
+    _attention(TYPES[dtype], 5, 4, 2, 100, 140, 64, causal=causal, q_lens=[100, 37, 0, 64, 1],
+               kv_lens=[140, 20, 77, 0, 65], garbage=garbage)
+
+
+@pytest.mark.parametrize("orders", [("bthd", "bhtd"), ("bhtd", "bthd"), ("tbhd", "htbd"), ("htbd", "tbhd")])
+def test_attention_memory_orders(orders):
+    _attention(torch.float16, 2, 6, 3, 66, 130, 72, causal=True, orders=orders, pad=24)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_sharp_and_flat_rows(dtype):
+    """Scores of +-100s (one key takes all), and scores that are all alike."""
+    _attention(TYPES[dtype], 1, 2, 1, 130, 200, 64, std=40.0, backward=False)
+    _attention(TYPES[dtype], 1, 2, 1, 130, 200, 64, std=0.0)
+    _attention(TYPES[dtype], 1, 2, 1, 130, 200, 64, scale=1e-3)
+
+
+@pytest.mark.parametrize("Q,K,H,G,D", [(700, 700, 8, 2, 128), (513, 1100, 4, 4, 64), (40, 2300, 4, 1, 96)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_longer(Q, K, H, G, D, dtype):
+    _attention(TYPES[dtype], 1, H, G, Q, K, D, causal=True, repeat=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("H,G,Q,D", [(1, 1, 1, 64), (8, 2, 1, 128), (16, 1, 1, 80), (7, 1, 2, 32), (4, 4, 16, 96),
+                                     (4, 1, 4, 40)])
+@pytest.mark.parametrize("K", [1, 31, 32, 33, 129, 511, 1025, 4000])
+def test_attention_few_rows(dtype, H, G, Q, D, K):
+    """Single tokens and small groups of them, over caches that are split or not."""
+    _attention(TYPES[dtype], 3, H, G, Q, K, D, causal=True, orders=("bthd", "bhtd"), backward=False,
+               kv_lens=[K, max(K // 3, 1), 0])
+
+
+def test_attention_keys_shared_by_the_batch():
+    """A batch stride of zero: one prefix for all requests (read only)."""
+    S = _S()
+    gen = _gen(5)
+    q = torch.randn(3, 4, 50, 64, generator=gen).to(torch.bfloat16)
+    k = torch.randn(1, 2, 90, 64, generator=gen).to(torch.bfloat16)
+    v = torch.randn(1, 2, 90, 64, generator=gen).to(torch.bfloat16)
+    want, tol = ref.attention(q, k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1), 0.125)
+    qd, kd, vd = q.cuda(), k.cuda().expand(3, -1, -1, -1), v.cuda().expand(3, -1, -1, -1)
+    o = torch.empty_like(qd)
+    S.attention_forward(S.attention_desc(qd, kd, vd, o), qd, kd, vd, o)
+    torch.cuda.synchronize()
+    ref.check("o", o, want["o"], tol["o"])
+
+
+def test_attention_cache_beyond_32_bits():
+    """A request whose keys lie more than 2^32 bytes into the cache, tokens far apart."""
+    S = _S()
+    B, G, K, D, pad = 3, 2, 70, 64, 1 << 14
+    cache = torch.zeros(B * 140 * 1024 * 1024 * 8, dtype=torch.bfloat16, device="cuda:0")  # 6.6 GiB
+    token, head, batch = D + pad, (D + pad) * K, 140 * 1024 * 1024 * 8
+    assert 2 * batch * (B - 1) > 2 ** 32 and head * G <= batch
+    gen = _gen(77)
+    k = torch.randn(B, G, K, D, generator=gen).to(torch.bfloat16)
+    v = torch.randn(B, G, K, D, generator=gen).to(torch.bfloat16)
+    kd = cache.as_strided((B, G, K, D), (batch, head, token, 1))
+    vd = cache.as_strided((B, G, K, D), (batch, head, token, 1), 1 << 13)
+    kd.copy_(k)
+    vd.copy_(v)
+    for Q in (1, 90):
+        q = torch.randn(B, 4, Q, D, generator=gen).to(torch.bfloat16)
+        do = torch.randn(B, 4, Q, D, generator=gen).to(torch.bfloat16)
+        want, tol = ref.attention(q, k, v, 0.125, dout=do)
+        qd, dod = q.cuda(), do.cuda()
+        o, dq = torch.empty_like(qd), torch.empty_like(qd)
+        lse = torch.empty(B, 4, Q, device="cuda:0")
+        dk, dv = torch.empty_like(k, device="cuda:0"), torch.empty_like(v, device="cuda:0")
+        d = S.attention_desc(qd, kd, vd, o, dq=dq, dk=dk, dv=dv)
+        ws = _scratch(max(S.attention_forward_scratch_bytes(d), S.attention_backward_scratch_bytes(d)))
+        S.attention_forward(d, qd, kd, vd, o, lse=lse, scratch=ws)
+        S.attention_backward(d, qd, kd, vd, o, dod, lse, dq, dk, dv, ws)
+        torch.cuda.synchronize()
+        for n, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+            ref.check(n, t, want[n], tol[n])
+
+
+def test_attention_backward_small_fp16_gradients():
+    """dout of the size that fp16 training meets without a loss scale: ds lies below fp16's range."""
+    S = _S()
+    gen = _gen(9)
+    Q = K = 300
+    q, k, v = ((torch.randn(1, 2, Q, 64, generator=gen)).to(torch.float16) for _ in range(3))
+    do = (torch.randn(1, 2, Q, 64, generator=gen) * 2e-4).to(torch.float16)
+    want, tol = ref.attention(q, k, v, 0.125, dout=do)
+    dev = [t.cuda() for t in (q, k, v, do)]
+    o, dq, dk, dv = (torch.empty_like(dev[0]) for _ in range(4))
+    lse = torch.empty(1, 2, Q, device="cuda:0")
+    d = S.attention_desc(dev[0], dev[1], dev[2], o)
+    ws = _scratch(max(S.attention_forward_scratch_bytes(d), S.attention_backward_scratch_bytes(d)))
+    S.attention_forward(d, dev[0], dev[1], dev[2], o, lse=lse, scratch=ws)
+    S.attention_backward(d, dev[0], dev[1], dev[2], o, dev[3], lse, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    for n, t in (("dv", dv), ("dk", dk), ("dq", dq)):
+        ref.check(n, t, want[n], tol[n])
+
+
+def test_attention_gradient_against_differences():
+    """<gradient, direction> against central differences of the 64-bit forward."""
+    S = _S()
+    gen = _gen(21)
+    q, k, v, do = (torch.randn(1, 2, 40, 32, generator=gen).to(torch.float16) for _ in range(4))
+    dev = [t.cuda() for t in (q, k, v, do)]
+    o, dq, dk, dv = (torch.empty_like(dev[0]) for _ in range(4))
+    lse = torch.empty(1, 2, 40, device="cuda:0")
+    d = S.attention_desc(*dev[:3], o, causal=True)
+    ws = _scratch(max(S.attention_forward_scratch_bytes(d), S.attention_backward_scratch_bytes(d)))
+    S.attention_forward(d, *dev[:3], o, lse=lse, scratch=ws)
+    S.attention_backward(d, *dev[:3], o, dev[3], lse, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    _, tol = ref.attention(q, k, v, 32 ** -0.5, True, dout=do)
+
+    def loss(*t):
+        return float((ref.attention(*t, 32 ** -0.5, True, dtype=torch.float16)[0]["o"] * do.double()).sum())
+
+    for i, (name, g) in enumerate((("dq", dq), ("dk", dk), ("dv", dv))):
+        way = torch.randn(g.shape, generator=gen).double()
+        ends = []
+        for h in (1e-4, -1e-4):
+            t = [q.double(), k.double(), v.double()]
+            t[i] = t[i] + h * way
+            ends.append(loss(*t))
+        diff = (ends[0] - ends[1]) / 2e-4
+        got = float((g.double().cpu() * way).sum())
+        # central differences: third derivatives times 1e-8
+        assert abs(got - diff) <= float((tol[name] * way.abs()).sum()) + 1e-6 * float(way.abs().sum()), (name, got, diff)
+
+
+# ---- linear ------------------------------------------------------------------------------------
+
+def _rows(t, pad=0):
+    """A matrix on the GPU, each row followed by `pad` elements of NaN."""
+    base = torch.full((t.shape[0], t.shape[1] + pad), NAN, dtype=t.dtype, device="cuda:0")
+    base[:, :t.shape[1]] = t
+    return base[:, :t.shape[1]]
+
+
+def _linear(dt, m, n, k, act="none", bias=True, residual=False, pad=0, dx_add=False, dw_fp32=False, backward=True):
+    S = _S()
+    gen = _gen(m, n, k)
+    x, w = torch.randn(m, k, generator=gen).to(dt), (torch.randn(n, k, generator=gen) * k ** -0.5 * 2).to(dt)
+    b = torch.randn(n, generator=gen) if bias else None
+    r = torch.randn(m, n, generator=gen).to(dt) if residual else None
+    want, tol = ref.linear(x, w, b, r, act)
+    xd, wd, y, z = _rows(x, pad), _rows(w, pad), _rows(torch.full((m, n), NAN, dtype=dt), pad), _rows(torch.full((m, n), NAN, dtype=dt), pad)
+    rd = None if r is None else _rows(r, pad)
+    print(f"[dnnseq] linear {dt} {m} x {n} x {k} {act}", flush=True)
+    desc = S.linear_desc(xd, wd, act, y=y, residual=rd, z=z)
+    S.linear_forward(desc, xd, wd, y, bias=None if b is None else b.cuda(), residual=rd, z=z,
+                     scratch=_scratch(S.linear_forward_scratch_bytes(desc)))
+    torch.cuda.synchronize()
+    ref.check("z", z, want["z"], tol["z"])
+    ref.check("y", y, want["y"], tol["y"])
+    if not backward:
+        return
+    dy = torch.randn(m, n, generator=gen).to(dt)
+    add = torch.randn(m, k, generator=gen).to(dt) if dx_add else None
+    zh = z.cpu()
+    want, tol = ref.linear_backward(x, w, dy, zh, add, act, dw_fp32)
+    dyd, dx = _rows(dy, pad), _rows(torch.full((m, k), NAN, dtype=dt), pad)
+    dw = _rows(torch.full((n, k), NAN, dtype=torch.float32 if dw_fp32 else dt), pad)
+    db = torch.full((n,), NAN, device="cuda:0")
+    addd = None if add is None else _rows(add, pad)
+    desc = S.linear_desc(xd, wd, act, z=z, dy=dyd, dx=dx, dx_add=addd, dw=dw)
+    S.linear_backward(desc, xd, wd, dyd, z=None if act == "none" else z, dx=dx, dx_add=addd, dw=dw, db=db,
+                      scratch=_scratch(S.linear_backward_scratch_bytes(desc)))
+    torch.cuda.synchronize()
+    for name, t in (("db", db), ("dx", dx), ("dw", dw)):
+        ref.check(name, t, want[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu", "mish"])
+def test_linear_activations(dtype, act):
+    _linear(TYPES[dtype], 77, 136, 200, act, residual=act == "gelu", dx_add=act == "silu", dw_fp32=act == "mish", pad=8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(1, 8, 8), (1, 1000, 264), (3, 64, 1032), (16, 72, 2048), (17, 512, 72), (33, 8, 4104),
+                                   (64, 264, 512), (65, 256, 512), (127, 128, 64), (128, 136, 128), (129, 264, 136),
+                                   (255, 640, 520), (256, 256, 256), (257, 776, 328), (600, 512, 1160), (1100, 520, 72)])
+def test_linear_shapes(dtype, m, n, k):
+    _linear(TYPES[dtype], m, n, k, "gelu", residual=m % 2 == 0, bias=m % 3 != 0, pad=16 * (m % 2), dx_add=m % 2 == 1)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 2048, 4096), (48, 1024, 8192), (2049, 256, 264), (4100, 72, 136)])
+def test_linear_long_contractions(m, n, k):
+    _linear(torch.bfloat16, m, n, k, "none", dw_fp32=True)
+
+
+def test_linear_in_place_residuals_and_parts():
+    """y over the residual, dx over dx_add, and calls that ask for one gradient only."""
+    S = _S()
+    gen = _gen(4)
+    for m, n, k in ((40, 96, 64), (300, 264, 2048)):
+        x, w = torch.randn(m, k, generator=gen).half(), torch.randn(n, k, generator=gen).half() / 16
+        r, dy, add = (torch.randn(m, c, generator=gen).half() for c in (n, n, k))
+        want, tol = ref.linear(x, w, None, r)
+        y = r.cuda()
+        desc = S.linear_desc(x.cuda(), w.cuda(), residual=y, y=y)
+        xd, wd, dyd = x.cuda(), w.cuda(), dy.cuda()
+        S.linear_forward(desc, xd, wd, y, residual=y, scratch=_scratch(S.linear_forward_scratch_bytes(desc)))
+        ref.check("y", y, want["y"], tol["y"])
+        want, tol = ref.linear_backward(x, w, dy, dx_add=add)
+        ws = _scratch(S.linear_backward_scratch_bytes(desc))
+        dx = add.cuda()
+        S.linear_backward(desc, xd, wd, dyd, dx=dx, dx_add=dx, scratch=ws)
+        ref.check("dx", dx, want["dx"], tol["dx"])
+        dw = torch.empty_like(wd)
+        S.linear_backward(desc, xd, None, dyd, dw=dw, scratch=ws)
+        ref.check("dw", dw, want["dw"], tol["dw"])
+        db = torch.empty(n, device="cuda:0")
+        S.linear_backward(desc, None, None, dyd, db=db, scratch=ws)
+        ref.check("db", db, want["db"], tol["db"])
+
+
+def test_linear_without_rows():
+    S = _S()
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda:0")
+    w = torch.ones(16, 64, dtype=torch.bfloat16, device="cuda:0")
+    y = torch.empty(0, 16, dtype=torch.bfloat16, device="cuda:0")
+    d = S.linear_desc(x, w, "gelu", y=y)
+    S.linear_forward(d, x, w, y)
+    dw, db = torch.full_like(w, NAN), torch.full((16,), NAN, device="cuda:0")
+    S.linear_backward(d, x, w, y, z=y, dx=x, dw=dw, db=db, scratch=_scratch(S.linear_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    assert (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu", "mish"])
+def test_linear_activation_tails(act):
+    """z far out on both sides, infinite and NaN, through an identity product."""
+    S = _S()
+    z = torch.tensor([0.0, -0.0, 1e-3, -1e-3, 20, -20, 21, -21, 60, -60, 90, -90, 300, -300, 3e4, -3e4,
+                      math.inf, NAN, 0.5, -0.5, 5, -5, 10, -10], dtype=torch.float64).to(torch.bfloat16)
+    n = z.numel()
+    w = torch.zeros(n, 8, dtype=torch.bfloat16)
+    w[:, 0] = z
+    x = torch.zeros(1, 8, dtype=torch.bfloat16)
+    x[0, 0] = 1
+    fin = z.isfinite()
+    w[~fin, 0] = 0
+    y, zo = torch.empty(1, n, dtype=torch.bfloat16, device="cuda:0"), torch.empty(1, n, dtype=torch.bfloat16, device="cuda:0")
+    d = S.linear_desc(x.cuda(), w.cuda(), act)
+    bias = torch.where(fin, torch.zeros(n), z.float()).cuda()  # (infinite times zero would be NaN)
+    S.linear_forward(d, x.cuda(), w.cuda(), y, bias=bias, z=zo, scratch=_scratch(S.linear_forward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    got, zz = y.double().cpu()[0], z.double()
+    want = ref.act(act, zz)
+    assert torch.equal(zo.cpu()[0][fin], z[fin]) and got[z.isnan()].isnan().all() and got[z == math.inf].eq(math.inf).all()
+    assert ((got - want)[fin].abs() <= 2.0 ** -7 * want[fin].abs() + 1e-6).all(), (got, want)
+    g = torch.ones(1, n, dtype=torch.bfloat16, device="cuda:0")
+    db = torch.empty(n, device="cuda:0")
+    S.linear_backward(d, None, None, g, z=zo, db=db, scratch=_scratch(S.linear_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    slope = ref.act_grad(act, zz)
+    assert ((db.double().cpu() - slope)[fin].abs() <= 64 * ref.E32 * (1 + zz[fin].abs().clamp_max(64))).all()
+    assert db.cpu()[z.isnan()].isnan().all()
+
+
+# ---- layer normalisation -----------------------------------------------------------------------
+
+NORM_SHAPES = [(1, 1), (3, 1), (5, 2), (4, 7), (9, 8), (17, 9), (33, 127), (40, 128), (3, 129), (7, 511), (5, 512),
+               (6, 513), (300, 1000), (4, 1024), (5, 1025), (70, 2048), (9, 2049), (600, 2500), (3, 4096), (5, 4097),
+               (2, 8192), (3, 8193), (2, 16383), (1, 16384), (1200, 264), (5000, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows,cols", NORM_SHAPES)
+@pytest.mark.parametrize("add", [False, True])
+def test_layernorm(dtype, rows, cols, add):
+    S, dt, eps = _S(), TYPES[dtype], 1e-5
+    gen = _gen(rows, cols, add)
+    pad = (rows + cols) % 3 * 5
+    x = (torch.randn(rows, cols, generator=gen) * 2 + 0.5).to(dt)
+    dy, a = torch.randn(rows, cols, generator=gen).to(dt), torch.randn(rows, cols, generator=gen).to(dt)
+    gamma, beta = 1 + 0.1 * torch.randn(cols, generator=gen), 0.1 * torch.randn(cols, generator=gen)
+    xd, dyd, ad = _rows(x, pad), _rows(dy, pad), _rows(a, pad) if add else None
+    y, dx = _rows(torch.full_like(x, NAN), pad), _rows(torch.full_like(x, NAN), pad)
+    mean, rstd = torch.full((rows,), NAN, device="cuda:0"), torch.full((rows,), NAN, device="cuda:0")
+    dg, db = torch.full((cols,), NAN, device="cuda:0"), torch.full((cols,), NAN, device="cuda:0")
+    print(f"[dnnseq] layernorm {dtype} {rows} x {cols} add={add}", flush=True)
+    d = S.layernorm_desc(xd, eps, y=y, dy=dyd, dx=dx, dx_add=ad)
+    S.layernorm_forward(d, xd, gamma.cuda(), beta.cuda(), y, mean, rstd)
+    ws = _scratch(S.layernorm_backward_scratch_bytes(d))
+    S.layernorm_backward(d, xd, dyd, gamma.cuda(), mean, rstd, dx, dg, db, ws, dx_add=ad)
+    torch.cuda.synchronize()
+    want, tol = ref.layernorm(x, gamma, beta, eps)
+    for n, t in (("mean", mean), ("rstd", rstd), ("y", y)):
+        ref.check(n, t, want[n], tol[n])
+    want, tol = ref.layernorm_backward(x, dy, gamma, eps, a if add else None)
+    for n, t in (("dx", dx), ("dgamma", dg), ("dbeta", db)):
+        ref.check(n, t, want[n], tol[n])
+    dg2, db2 = torch.empty_like(dg), torch.empty_like(db)
+    S.layernorm_backward(d, xd, dyd, gamma.cuda(), mean, rstd, dx, dg2, db2, ws, dx_add=ad)
+    torch.cuda.synchronize()
+    assert torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
+def test_layernorm_rows_far_from_zero_and_no_rows():
+    """A mean a thousand times the deviation (the variance is taken about the mean), and no rows."""
+    S = _S()
+    gen = _gen(3)
+    for cols in (96, 1000, 4000, 9000):
+        x = (torch.randn(4, cols, generator=gen) + 1000).to(torch.float16)
+        gamma, beta = torch.ones(cols), torch.zeros(cols)
+        xd = x.cuda()
+        y, mean, rstd = torch.empty_like(xd), torch.empty(4, device="cuda:0"), torch.empty(4, device="cuda:0")
+        S.layernorm_forward(S.layernorm_desc(xd), xd, gamma.cuda(), beta.cuda(), y, mean, rstd)
+        want, _ = ref.layernorm(x, gamma, beta, 1e-5)
+        # the mean is off by some e32 of 1000, a ten-thousandth of the deviation, each y by no more
+        # than that and its rounding
+        assert (y.double().cpu() - want["y"]).abs().max() <= 1e-3 + 2.0 ** -11 * want["y"].abs().max()
+        assert ((rstd.double().cpu() - want["rstd"]).abs() <= 1e-4 * want["rstd"]).all()
+    x = torch.empty(0, 40, dtype=torch.float16, device="cuda:0")
+    dg, db = torch.full((40,), NAN, device="cuda:0"), torch.full((40,), NAN, device="cuda:0")
+    e = torch.empty(0, device="cuda:0")
+    d = S.layernorm_desc(x)
+    S.layernorm_forward(d, x, dg, db, x, e, e)
+    S.layernorm_backward(d, x, x, torch.ones(40, device="cuda:0"), e, e, x, dg, db, None)
+    torch.cuda.synchronize()
+    assert (dg == 0).all() and (db == 0).all()
+
+
+def test_layernorm_in_place_gradient():
+    S = _S()
+    gen = _gen(31)
+    x, dy, a = (torch.randn(50, 2056, generator=gen).to(torch.bfloat16) for _ in range(3))
+    gamma = 1 + 0.1 * torch.randn(2056, generator=gen)
+    want, tol = ref.layernorm_backward(x, dy, gamma, 1e-5, a)
+    xd, dx = x.cuda(), a.cuda()
+    mean, rstd = torch.empty(50, device="cuda:0"), torch.empty(50, device="cuda:0")
+    y, dg = torch.empty_like(xd), torch.empty(2056, device="cuda:0")
+    d = S.layernorm_desc(xd)
+    S.layernorm_forward(d, xd, gamma.cuda(), torch.zeros(2056, device="cuda:0"), y, mean, rstd)
+    db = torch.empty_like(dg)
+    S.layernorm_backward(d, xd, dy.cuda(), gamma.cuda(), mean, rstd, dx, dg, db,
+                         _scratch(S.layernorm_backward_scratch_bytes(d)), dx_add=dx)
+    torch.cuda.synchronize()
+    ref.check("dx", dx, want["dx"], tol["dx"])
