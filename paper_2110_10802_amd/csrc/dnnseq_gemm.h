@@ -6,10 +6,10 @@
 //          the forward product, dy in the data gradient
 //   across the contraction runs over its rows (ld elements apart): w in the data gradient, both
 //          operands of the weight gradient
-// A step takes 64 elements of the contraction.  Both tiles go from memory straight into LDS, 16
+// A step takes 64 elements of the contraction, in two halves of 32.  Both tiles go from memory straight into LDS, 16
 // bytes per lane; what lies past the operand's end arrives as zeros (a bounded buffer, lanes past a
-// row's end sent out of bounds).  LDS holds rows of 128 bytes (along) or TILE * 2 bytes (across) as
-// memory has them, 16-byte units permuted within a row so that the reads spread over the banks:
+// row's end sent out of bounds).  LDS holds rows of 128 bytes (along: whole lines of the caches) or TILE * 2 bytes (across) as
+// memory has them, 16-byte units permuted within a row so that the reads meet the 64 banks evenly:
 //   along   unit u of row r at u ^ (r & 7); a lane reads 8 consecutive c of its row (ds_read_b128)
 //   across  unit pair v of row c at v ^ ((c & 3) | (c >> 3 & 1) << 2); two transposing reads give a
 //           lane 8 consecutive c of its column
@@ -65,12 +65,12 @@ struct Loader {
                 off[i] = kNowhere;
         }
     }
-    // left: elements of the contraction from this step's start
+    // left: elements of the contraction from this step's start; none: no memory is read
     __device__ __forceinline__ void load(char *lds, int left)
     {
-        const uint32_t rows = ACROSS ? min(left, kStep) : limit;
-        const uint32_t last = (ACROSS ? width : min(left, kStep)) * 2;
-        const auto r = buffer(base, (rows - 1) * ld + last);
+        const int rows = ACROSS ? min(left, kStep) : limit;
+        const int last = (ACROSS ? width : min(left, kStep)) * 2;
+        const auto r = buffer(base, ((uint32_t)(rows - 1) * ld + last) & (0u - (uint32_t)(left > 0)));
         const uint32_t w0 = wave_id() * (kWave * 16);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -100,10 +100,10 @@ struct Reader {
                 off[f] = (g * 8 + i / 4) * (TILE * 2) + ((pair & ~7) | ((pair & 7) ^ s)) * 32 + i % 4 * 8;
             }
         } else {
-            off[0] = (first + i) * 128 + ((g ^ (i & 7)) * 16);
+            off[0] = (first + i) * 128 + (g ^ (i & 7)) * 16;
         }
     }
-    // fragment f (rows first + 16 f ..), half kk of the step
+    // fragment f (rows first + 16 f ..) of half kk
     __device__ __forceinline__ u32x4 get(const char *lds, int f, int kk) const
     {
         if (ACROSS) {

@@ -27,13 +27,35 @@ struct Product {
     float *partial;     // [splits][nq][np], instead of the epilogue
 };
 
-__device__ __forceinline__ float activation(int act, float z)
+// 1 - Phi(|z|) = exp(-z^2/2) E/2 with E = erfcx(|z|/sqrt 2) as t times a polynomial in t = 1/(1 + 0.3005 |z|)
+// (fitted to 1.5e-7 of E for |z| <= 14; beyond, the exponential is below 1e-42).  erff costs three
+// times as many instructions, and an epilogue of 65536 elements per CU has nothing to hide them behind.
+__device__ __forceinline__ float normal_tail(float z, float &gauss)
 {
-    switch (act) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.30052039f, fabsf(z), 1.0f));
+    float p = 0.071479224f;
+    p = fmaf(p, t, -0.31316078f);
+    p = fmaf(p, t, 0.40762401f);
+    p = fmaf(p, t, -0.10325651f);
+    p = fmaf(p, t, 0.25508931f);
+    p = fmaf(p, t, 0.20070525f);
+    p = fmaf(p, t, 0.24184074f);
+    p = fmaf(p, t, 0.23967862f);
+    gauss = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+    return 0.5f * gauss * t * p;
+}
+
+template <int ACT>
+__device__ __forceinline__ float activation(float z)
+{
+    switch (ACT) {
     case DNNSEQ_ACT_RELU:
         return z < 0.f ? 0.f : z; // (NaN stays NaN)
-    case DNNSEQ_ACT_GELU:
-        return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    case DNNSEQ_ACT_GELU: {
+        float gauss;
+        const float h = normal_tail(z, gauss);
+        return z * (z < 0.f ? h : 1.0f - h);
+    }
     case DNNSEQ_ACT_SILU:
         // -z beyond 126 log 2: the exponential's reciprocal is denormal; the product is below 1e-36
         return z * mbk::sigmoidf_fast(z);
@@ -46,13 +68,19 @@ __device__ __forceinline__ float activation(int act, float z)
     return z;
 }
 
-__device__ __forceinline__ float activation_grad(int act, float z)
+template <int ACT>
+__device__ __forceinline__ float activation_grad(float z)
 {
-    switch (act) {
+    switch (ACT) {
+    case DNNSEQ_ACT_NONE:
+        break;
     case DNNSEQ_ACT_RELU:
         return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    case DNNSEQ_ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    case DNNSEQ_ACT_GELU: {
+        float gauss;
+        const float h = normal_tail(z, gauss);
+        return fmaf(z * 0.39894228040143268f, gauss, z < 0.f ? h : 1.0f - h);
+    }
     case DNNSEQ_ACT_SILU: {
         const float s = mbk::sigmoidf_fast(z);
         return s * (1.0f + z * (1.0f - s));
@@ -66,26 +94,69 @@ __device__ __forceinline__ float activation_grad(int act, float z)
     return 1.f;
 }
 
-// Four consecutive p of row q: bias, z, activation, what is added, and the store.
-template <class T>
-__device__ __forceinline__ void finish(const Product &a, int q, int p, f32x4 v)
+struct Eight {
+    float v[8];
+};
+__device__ __forceinline__ Eight load8(const float *p)
 {
-    if (a.bias)
-        v += *(const f32x4 *)(a.bias + p);
-    if (a.z)
-        *(u32x2 *)((uint16_t *)a.z + q * a.ldz + p) = u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
-    if (a.act)
+    const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+    return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+__device__ __forceinline__ void store8(float *p, const Eight &e)
+{
+    *(f32x4 *)p = f32x4{e.v[0], e.v[1], e.v[2], e.v[3]};
+    *(f32x4 *)(p + 4) = f32x4{e.v[4], e.v[5], e.v[6], e.v[7]};
+}
+template <class T>
+__device__ __forceinline__ u32x4 round8(const Eight &e)
+{
+    return u32x4{T::pack(e.v[0], e.v[1]), T::pack(e.v[2], e.v[3]), T::pack(e.v[4], e.v[5]), T::pack(e.v[6], e.v[7])};
+}
+
+// Eight consecutive p of row q: z, activation, what is added, and the store.  `e` holds the products,
+// `bias` the bias there (or zeros).
+template <class T>
+__device__ __forceinline__ void finish(const Product &a, int64_t q, int p, Eight e, const Eight &bias)
+{
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            v[r] = activation(a.act, v[r]);
+    for (int i = 0; i < 8; ++i)
+        e.v[i] += bias.v[i];
+    if (a.z)
+        *(u32x4 *)((uint16_t *)a.z + q * a.ldz + p) = round8<T>(e);
+    switch (a.act) { // (the same for the whole launch)
+    case DNNSEQ_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            e.v[i] = activation<DNNSEQ_ACT_RELU>(e.v[i]);
+        break;
+    case DNNSEQ_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            e.v[i] = activation<DNNSEQ_ACT_GELU>(e.v[i]);
+        break;
+    case DNNSEQ_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            e.v[i] = activation<DNNSEQ_ACT_SILU>(e.v[i]);
+        break;
+    case DNNSEQ_ACT_MISH:
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            e.v[i] = activation<DNNSEQ_ACT_MISH>(e.v[i]);
+        break;
+    }
     if (a.add) {
-        const u32x2 w = *(const u32x2 *)((const uint16_t *)a.add + q * a.ldadd + p);
-        v += f32x4{T::lo(w[0]), T::hi(w[0]), T::lo(w[1]), T::hi(w[1])};
+        const u32x4 w = *(const u32x4 *)((const uint16_t *)a.add + q * a.ldadd + p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e.v[2 * i] += T::lo(w[i]);
+            e.v[2 * i + 1] += T::hi(w[i]);
+        }
     }
     if (a.out32)
-        *(f32x4 *)((float *)a.out + q * a.ldo + p) = v;
+        store8((float *)a.out + q * a.ldo + p, e);
     else
-        *(u32x2 *)((uint16_t *)a.out + q * a.ldo + p) = u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+        *(u32x4 *)((uint16_t *)a.out + q * a.ldo + p) = round8<T>(e);
 }
 
 // Tiles in the order of workgroups: the eight XCDs (workgroup b runs on XCD b % 8) take runs of
@@ -100,30 +171,46 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t n, uint32_t np, uin
     tp = r / rows;
 }
 
-// One step: the next step's tiles are requested, this one's multiplied.  (The two buffers are
-// restrict arguments: without that every read of LDS waits for the loads into the other buffer.)
-template <class T, class LP, class LQ, class RP, class RQ, int FP, int FQ, int QOFF>
-__device__ __forceinline__ void product_step(const char *__restrict__ cur, char *__restrict__ nxt, LP &lp, LQ &lq,
-                                             const RP &rp, const RQ &rq, f32x4 (&acc)[FP][FQ], int left)
+// Half a step multiplies fragments that are in registers already while it reads the next half's from LDS,
+// so the matrix cores have work from the barrier on.  (What is read and what is loaded into are restrict
+// arguments: without that every read of LDS waits for all loads into it.)
+template <class T, class RP, class RQ, int FP, int FQ, int QOFF>
+__device__ __forceinline__ void product_read(const char *__restrict__ buf, const RP &rp, const RQ &rq, int kk,
+                                             u32x4 (&fp)[FP], u32x4 (&fq)[FQ])
 {
-    if (left > 0) {
-        lp.load(nxt, left);
-        lq.load(nxt + QOFF, left);
-    }
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-        u32x4 fp[FP], fq[FQ];
+    for (int i = 0; i < FP; ++i)
+        fp[i] = rp.get(buf, i, kk);
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+        fq[j] = rq.get(buf + QOFF, j, kk);
+}
+template <class T, int FP, int FQ>
+__device__ __forceinline__ void product_multiply(const u32x4 (&fp)[FP], const u32x4 (&fq)[FQ], f32x4 (&acc)[FP][FQ])
+{
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
 #pragma unroll
         for (int i = 0; i < FP; ++i)
-            fp[i] = rp.get(cur, i, kk);
-#pragma unroll
-        for (int j = 0; j < FQ; ++j)
-            fq[j] = rq.get(cur + QOFF, j, kk);
-#pragma unroll
-        for (int j = 0; j < FQ; ++j)
-#pragma unroll
-            for (int i = 0; i < FP; ++i)
-                acc[i][j] = T::mma16(fp[i], fq[j], acc[i][j]);
+            acc[i][j] = T::mma16(fp[i], fq[j], acc[i][j]);
+}
+
+// The order of half a step in the instruction stream: reads of LDS spread over the first three quarters
+// of the products, so that the last of them have arrived at its end, loads from memory over the first
+// half.
+constexpr int due(int i, int n, int over) { return i < over ? (i * n + over - 1) / over : n; }
+template <int READS, int PRODUCTS, int LOADS, int I = 0>
+__device__ __forceinline__ void interleave()
+{
+    if constexpr (I < PRODUCTS) {
+        constexpr int R = due(I + 1, READS, PRODUCTS * 3 / 4) - due(I, READS, PRODUCTS * 3 / 4);
+        constexpr int L = due(I + 1, LOADS, PRODUCTS / 2) - due(I, LOADS, PRODUCTS / 2);
+        if constexpr (R > 0)
+            __builtin_amdgcn_sched_group_barrier(0x100, R, 0); // LDS reads
+        if constexpr (L > 0)
+            __builtin_amdgcn_sched_group_barrier(0x020, L, 0); // loads
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // a product
+        interleave<READS, PRODUCTS, LOADS, I + 1>();
     }
 }
 
@@ -139,8 +226,7 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
     uint32_t tp, tq;
     tile_of(blockIdx.x, np * nq, np, nq, tp, tq);
     const int p0 = tp * TP, q0 = tq * TQ;
-    const int c0 = blockIdx.y * a.steps * kStep, left = a.nc - c0;
-    const int steps = min(a.steps, (left + kStep - 1) / kStep);
+    const int c0 = blockIdx.y * a.steps * kStep, left = min(a.nc - c0, a.steps * kStep);
     Loader<PX, TP, THREADS> lp;
     Loader<QX, TQ, THREADS> lq;
     lp.init(a.p, a.ldp, p0, a.np, c0);
@@ -157,32 +243,76 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
 #pragma unroll
         for (int j = 0; j < FQ; ++j)
             acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (steps > 0) {
-        lp.load(lds, left);
-        lq.load(lds + LP::kBytes, left);
+    u32x4 fp[2][FP], fq[2][FQ];
+    typedef Reader<PX, TP> RP;
+    typedef Reader<QX, TQ> RQ;
+    constexpr int READS = FP * (PX ? 2 : 1) + FQ * (QX ? 2 : 1);
+    constexpr int LOADS = Loader<PX, TP, THREADS>::kLoads + Loader<QX, TQ, THREADS>::kLoads;
+    // This wavefront's loads into LDS have landed and it has read what it wanted; past the barrier that
+    // holds for all.
+    const auto landed = [] __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    const auto load = [&](char *__restrict__ buf, int s) __attribute__((always_inline)) {
+        lp.load(buf, left - s * kStep);
+        lq.load(buf + LP::kBytes, left - s * kStep);
+    };
+    const auto first_half = [&](const char *__restrict__ cur) __attribute__((always_inline)) {
+        product_read<T, RP, RQ, FP, FQ, LP::kBytes>(cur, rp, rq, 1, fp[1], fq[1]);
+        product_multiply<T, FP, FQ>(fp[0], fq[0], acc);
+        interleave<READS, FP * FQ, 0>();
+    };
+    const auto second_half = [&](char *__restrict__ cur, const char *__restrict__ nxt, int s)
+                                 __attribute__((always_inline)) {
+        load(cur, s + 2);
+        product_read<T, RP, RQ, FP, FQ, LP::kBytes>(nxt, rp, rq, 0, fp[0], fq[0]);
+        product_multiply<T, FP, FQ>(fp[1], fq[1], acc);
+        interleave<READS, FP * FQ, LOADS>();
+    };
+    load(lds, 0);
+    load(lds + BUF, 1);
+    landed();
+    product_read<T, RP, RQ, FP, FQ, LP::kBytes>(lds, rp, rq, 0, fp[0], fq[0]);
+    for (int s = 0; s * kStep < left; ++s) {
+        char *cur = lds + (s & 1) * BUF, *nxt = lds + (~s & 1) * BUF;
+        __builtin_amdgcn_sched_barrier(0);
+        first_half(cur);
+        landed();
+        second_half(cur, nxt, s);
     }
-    for (int s = 0; s < steps; ++s) {
-        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
-        __syncthreads();                    // and everyone's; the other buffer is no longer read
-        product_step<T, Loader<PX, TP, THREADS>, Loader<QX, TQ, THREADS>, Reader<PX, TP>, Reader<QX, TQ>, FP, FQ,
-                     LP::kBytes>(lds + (s & 1) * BUF, lds + (~s & 1) * BUF, lp, lq, rp, rq, acc,
-                                 s + 1 < steps ? left - (s + 1) * kStep : 0);
-    }
-    const int lane = threadIdx.x % kWave;
+    // Epilogue: a wavefront turns 16 rows q at a time through its own part of LDS, so that a lane holds
+    // eight consecutive p and rows are written in whole lines (8 scattered bytes per lane straight from the
+    // accumulators cost 16 us more for 2 x 32 MB).  The pitch of 4 floats past the row spreads the writes
+    // over the banks.
+    __builtin_amdgcn_s_waitcnt(0x0f70); // no load into LDS is on its way
+    __syncthreads();
+    constexpr int WIDE = TP / WP, PITCH = WIDE + 4, LANES = WIDE / 8, ROWS = kWave / LANES;
+    static_assert(16 * PITCH * 4 * WP * WQ <= 2 * BUF, "a wavefront's rows fit its part of LDS");
+    float *mine = (float *)lds + w * (16 * PITCH);
+    const int lane = threadIdx.x % kWave, p = p0 + wp + lane % LANES * 8;
+    Eight bias = {};
+    if (a.bias && !a.partial && p < a.np)
+        bias = load8(a.bias + p);
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
-        const int q = q0 + wq + j * 16 + lane % 16;
-        if (q >= a.nq)
-            continue;
 #pragma unroll
-        for (int i = 0; i < FP; ++i) {
-            const int p = p0 + wp + i * 16 + lane / 16 * 4;
-            if (p >= a.np)
+        for (int i = 0; i < FP; ++i)
+            *(f32x4 *)(mine + lane % 16 * PITCH + i * 16 + lane / 16 * 4) = acc[i][j];
+#pragma unroll 2
+        for (int r = lane / LANES; r < 16; r += ROWS) {
+            const int q = q0 + wq + j * 16 + r;
+            const Eight e = load8(mine + r * PITCH + lane % LANES * 8);
+            if (q >= a.nq || p >= a.np)
                 continue;
             if (a.partial)
-                *(f32x4 *)(a.partial + ((size_t)blockIdx.y * a.nq + q) * a.np + p) = acc[i][j];
+                store8(a.partial + ((size_t)blockIdx.y * a.nq + q) * a.np + p, e);
             else
-                finish<T>(a, q, p, acc[i][j]);
+                finish<T>(a, q, p, e, bias);
         }
     }
 }
@@ -191,13 +321,18 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
 template <class T>
 __global__ __launch_bounds__(256) void product_finish_kernel(Product a, int splits)
 {
-    const size_t quads = (size_t)a.nq * (a.np / 4), plane = (size_t)a.nq * a.np;
-    for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < quads; i += (size_t)gridDim.x * 256) {
-        f32x4 v = *(const f32x4 *)(a.partial + i * 4);
-        for (int s = 1; s < splits; ++s)
-            v += *(const f32x4 *)(a.partial + s * plane + i * 4);
-        const int q = (int)(i / (a.np / 4));
-        finish<T>(a, q, (int)(i * 4 - (size_t)q * a.np), v);
+    const uint32_t units = a.np / 8;
+    const size_t all = (size_t)a.nq * units, plane = (size_t)a.nq * a.np;
+    for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
+        Eight e = load8(a.partial + i * 8);
+        for (int s = 1; s < splits; ++s) {
+            const Eight f = load8(a.partial + s * plane + i * 8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                e.v[j] += f.v[j];
+        }
+        const uint32_t q = (uint32_t)(i / units), p = (uint32_t)(i - (size_t)q * units) * 8;
+        finish<T>(a, q, p, e, a.bias ? load8(a.bias + p) : Eight{});
     }
 }
 
@@ -205,9 +340,9 @@ __global__ __launch_bounds__(256) void product_finish_kernel(Product a, int spli
 // columns, wavefront: every fourth row), column sums in fp32 before g is rounded, one partial row
 // per 64 rows.
 constexpr int kGradRows = 64;
-template <class T>
+template <class T, int ACT>
 __global__ __launch_bounds__(256) void act_grad_kernel(const void *dy, int64_t lddy, const void *z, int64_t ldz,
-                                                       int act, int m, int n, void *g, float *psum)
+                                                       int m, int n, void *g, float *psum)
 {
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
     const int c = (blockIdx.x * kWave + lane) * 4, r0 = blockIdx.y * kGradRows;
@@ -217,12 +352,12 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const void *dy, int64_t l
         for (int r = r0 + w; r < min(r0 + kGradRows, m); r += 4) {
             const u32x2 d = *(const u32x2 *)((const uint16_t *)dy + r * lddy + c);
             f32x4 v = {T::lo(d[0]), T::hi(d[0]), T::lo(d[1]), T::hi(d[1])};
-            if (act) {
+            if (ACT) {
                 const u32x2 e = *(const u32x2 *)((const uint16_t *)z + r * ldz + c);
                 const f32x4 t = {T::lo(e[0]), T::hi(e[0]), T::lo(e[1]), T::hi(e[1])};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    v[i] *= activation_grad(act, t[i]);
+                    v[i] *= activation_grad<ACT>(t[i]);
                 *(u32x2 *)((uint16_t *)g + (size_t)r * n + c) = u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
             }
             s += v;
@@ -263,17 +398,21 @@ int splits_for(int np, int nq, int nc, int tile)
 template <class T, bool PX, bool QX>
 hipError_t launch_product(Product a, float *scratch, hipStream_t st)
 {
-    constexpr int TILE = 128;
+    const bool big = ((a.np + 255) / 256) * ((a.nq + 255) / 256) >= 200;
+    const int TILE = big ? 256 : 128;
     const int splits = splits_for(a.np, a.nq, a.nc, TILE);
     const int steps = (a.nc + kStep - 1) / kStep;
     a.steps = (steps + splits - 1) / splits;
     const int used = std::max(1, (steps + a.steps - 1) / std::max(a.steps, 1));
     a.partial = used > 1 ? scratch : nullptr;
     const dim3 grid(((a.np + TILE - 1) / TILE) * ((a.nq + TILE - 1) / TILE), used);
-    product_kernel<T, PX, QX, TILE, TILE, 2, 2><<<grid, 256, 0, st>>>(a);
+    if (big)
+        product_kernel<T, PX, QX, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
+    else
+        product_kernel<T, PX, QX, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
     if (used > 1) {
-        const size_t quads = (size_t)a.nq * (a.np / 4);
-        product_finish_kernel<T><<<(unsigned)std::min<size_t>((quads + 255) / 256, 4096), 256, 0, st>>>(a, used);
+        const size_t units = (size_t)a.nq * (a.np / 8);
+        product_finish_kernel<T><<<(unsigned)std::min<size_t>((units + 255) / 256, 4096), 256, 0, st>>>(a, used);
     }
     return hipGetLastError();
 }
@@ -322,8 +461,25 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
     int64_t ldg = d.lddy;
     const int parts = (d.m + kGradRows - 1) / kGradRows;
     if ((d.activation || db) && d.m) {
-        act_grad_kernel<T><<<dim3((d.n + 255) / 256, parts), 256, 0, st>>>(
-            dy, d.lddy, z, d.ldz, d.activation, d.m, d.n, ws + l.g, db ? (float *)(ws + l.psum) : nullptr);
+        const dim3 grid((d.n + 255) / 256, parts);
+        float *psum = db ? (float *)(ws + l.psum) : nullptr;
+        const auto grad = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(dy, d.lddy, z, d.ldz, d.m, d.n, ws + l.g, psum); };
+        switch (d.activation) {
+        case DNNSEQ_ACT_RELU:
+            grad(act_grad_kernel<T, DNNSEQ_ACT_RELU>);
+            break;
+        case DNNSEQ_ACT_GELU:
+            grad(act_grad_kernel<T, DNNSEQ_ACT_GELU>);
+            break;
+        case DNNSEQ_ACT_SILU:
+            grad(act_grad_kernel<T, DNNSEQ_ACT_SILU>);
+            break;
+        case DNNSEQ_ACT_MISH:
+            grad(act_grad_kernel<T, DNNSEQ_ACT_MISH>);
+            break;
+        default:
+            grad(act_grad_kernel<T, DNNSEQ_ACT_NONE>);
+        }
         if (d.activation) {
             g = ws + l.g;
             ldg = d.n;
