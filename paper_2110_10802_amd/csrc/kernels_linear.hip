@@ -174,7 +174,7 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t n, uint32_t np, uin
 // Half a step multiplies fragments that are in registers already while it reads the next half's from LDS,
 // so the matrix cores have work from the barrier on.  (What is read and what is loaded into are restrict
 // arguments: without that every read of LDS waits for all loads into it.)
-template <class T, class RP, class RQ, int FP, int FQ, int QOFF>
+template <class RP, class RQ, int FP, int FQ, int QOFF>
 __device__ __forceinline__ void product_read(const char *__restrict__ buf, const RP &rp, const RQ &rq, int kk,
                                              u32x4 (&fp)[FP], u32x4 (&fq)[FQ])
 {
@@ -214,14 +214,15 @@ __device__ __forceinline__ void interleave()
     }
 }
 
-template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ>
+template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF>
 __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
 {
     constexpr int THREADS = WP * WQ * kWave, FP = TP / WP / 16, FQ = TQ / WQ / 16;
     typedef Tile<PX, TP> LP;
     typedef Tile<QX, TQ> LQ;
     constexpr int BUF = LP::kBytes + LQ::kBytes;
-    __shared__ __attribute__((aligned(256))) char lds[2 * BUF]; // [2][P tile, Q tile]
+    static_assert((NBUF & (NBUF - 1)) == 0 || NBUF == 3, "buffers");
+    __shared__ __attribute__((aligned(256))) char lds[NBUF * BUF]; // [NBUF][P tile, Q tile]
     const uint32_t np = (a.np + TP - 1) / TP, nq = (a.nq + TQ - 1) / TQ;
     uint32_t tp, tq;
     tile_of(blockIdx.x, np * nq, np, nq, tp, tq);
@@ -248,12 +249,14 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
     typedef Reader<QX, TQ> RQ;
     constexpr int READS = FP * (PX ? 2 : 1) + FQ * (QX ? 2 : 1);
     constexpr int LOADS = Loader<PX, TP, THREADS>::kLoads + Loader<QX, TQ, THREADS>::kLoads;
-    // This wavefront's loads into LDS have landed and it has read what it wanted; past the barrier that
-    // holds for all.
+    // Of this wavefront's loads into LDS no more than those of the last NBUF - 2 steps are on their way,
+    // and it has read what it wanted; past the barrier that holds for all.
+    constexpr int AHEAD = (NBUF - 2) * LOADS;
+    static_assert(AHEAD < 64, "vmcnt");
     const auto landed = [] __attribute__((always_inline)) {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (AHEAD & 15) | (AHEAD >> 4) << 14); // vmcnt(AHEAD), lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
@@ -263,27 +266,29 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
         lq.load(buf + LP::kBytes, left - s * kStep);
     };
     const auto first_half = [&](const char *__restrict__ cur) __attribute__((always_inline)) {
-        product_read<T, RP, RQ, FP, FQ, LP::kBytes>(cur, rp, rq, 1, fp[1], fq[1]);
+        product_read<RP, RQ, FP, FQ, LP::kBytes>(cur, rp, rq, 1, fp[1], fq[1]);
         product_multiply<T, FP, FQ>(fp[0], fq[0], acc);
         interleave<READS, FP * FQ, 0>();
     };
     const auto second_half = [&](char *__restrict__ cur, const char *__restrict__ nxt, int s)
                                  __attribute__((always_inline)) {
-        load(cur, s + 2);
-        product_read<T, RP, RQ, FP, FQ, LP::kBytes>(nxt, rp, rq, 0, fp[0], fq[0]);
+        load(cur, s + NBUF);
+        product_read<RP, RQ, FP, FQ, LP::kBytes>(nxt, rp, rq, 0, fp[0], fq[0]);
         product_multiply<T, FP, FQ>(fp[1], fq[1], acc);
         interleave<READS, FP * FQ, LOADS>();
     };
-    load(lds, 0);
-    load(lds + BUF, 1);
+    for (int s = 0; s < NBUF; ++s)
+        load(lds + s * BUF, s);
     landed();
-    product_read<T, RP, RQ, FP, FQ, LP::kBytes>(lds, rp, rq, 0, fp[0], fq[0]);
+    product_read<RP, RQ, FP, FQ, LP::kBytes>(lds, rp, rq, 0, fp[0], fq[0]);
+    uint32_t at = 0;
     for (int s = 0; s * kStep < left; ++s) {
-        char *cur = lds + (s & 1) * BUF, *nxt = lds + (~s & 1) * BUF;
+        const uint32_t next = at == (NBUF - 1) * BUF ? 0 : at + BUF;
         __builtin_amdgcn_sched_barrier(0);
-        first_half(cur);
+        first_half(lds + at);
         landed();
-        second_half(cur, nxt, s);
+        second_half(lds + at, lds + next, s);
+        at = next;
     }
     // Epilogue: a wavefront turns 16 rows q at a time through its own part of LDS, so that a lane holds
     // eight consecutive p and rows are written in whole lines (8 scattered bytes per lane straight from the
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
     __builtin_amdgcn_s_waitcnt(0x0f70); // no load into LDS is on its way
     __syncthreads();
     constexpr int WIDE = TP / WP, PITCH = WIDE + 4, LANES = WIDE / 8, ROWS = kWave / LANES;
-    static_assert(16 * PITCH * 4 * WP * WQ <= 2 * BUF, "a wavefront's rows fit its part of LDS");
+    static_assert(16 * PITCH * 4 * WP * WQ <= NBUF * BUF, "a wavefront's rows fit its part of LDS");
     float *mine = (float *)lds + w * (16 * PITCH);
     const int lane = threadIdx.x % kWave, p = p0 + wp + lane % LANES * 8;
     Eight bias = {};
@@ -336,90 +341,211 @@ __global__ __launch_bounds__(256) void product_finish_kernel(Product a, int spli
     }
 }
 
-// g = dy act'(z) and the sums of its columns: a workgroup takes 64 rows x 256 columns (lane: four
-// columns, wavefront: every fourth row), column sums in fp32 before g is rounded, one partial row
-// per 64 rows.
+// Few rows q (at most 16 FQ): bound by reading the p operand once, and for small ones by latency.  A
+// workgroup takes 16 p and the whole contraction; its eight wavefronts take every eighth 32 elements, so
+// together they read 512 bytes of each of the 16 rows at a time, straight into operand order, UNROLL of
+// those on the way per wavefront.  No second launch: the wavefronts' sums meet in LDS.
+template <class T, int FQ>
+__global__ __launch_bounds__(512) void product_rows_kernel(Product a)
+{
+    constexpr int UNROLL = FQ == 1 ? 8 : 4, W = 8, PITCH = 20;
+    __shared__ __attribute__((aligned(16))) float red[W][16 * FQ][PITCH];
+    const int lane = threadIdx.x % kWave, w = wave_id(), i = lane % 16, g = lane / 16;
+    const int p0 = blockIdx.x * 16;
+    const uint32_t ldp = (uint32_t)a.ldp * 2, ldq = (uint32_t)a.ldq * 2;
+    const auto rp = buffer((const uint16_t *)a.p + p0 * a.ldp, (uint32_t)(min(a.np - p0, 16) - 1) * ldp + a.nc * 2);
+    const auto rq = buffer(a.q, (uint32_t)(a.nq - 1) * ldq + a.nc * 2);
+    f32x4 acc[FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+        acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c0 = w * 32; c0 < a.nc; c0 += UNROLL * W * 32) {
+        u32x4 fp[UNROLL], fq[UNROLL][FQ];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int c = c0 + u * (W * 32) + g * 8; // (past the end: no memory is read)
+            fp[u] = __builtin_bit_cast(
+                u32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, c < a.nc ? i * ldp + c * 2 : kNowhere, 0, 0));
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                fq[u][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                         rq, c < a.nc ? (i + 16 * j) * ldq + c * 2 : kNowhere, 0, 0));
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                acc[j] = T::mma16(fp[u], fq[u][j], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+        *(f32x4 *)&red[w][j * 16 + i][g * 4] = acc[j];
+    __syncthreads();
+    const int q = threadIdx.x / 2, half = threadIdx.x % 2 * 8, p = p0 + half;
+    if (q >= min(a.nq, 16 * FQ) || p >= a.np)
+        return;
+    Eight e = load8(&red[0][q][half]);
+#pragma unroll
+    for (int v = 1; v < W; ++v) {
+        const Eight f = load8(&red[v][q][half]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            e.v[k] += f.v[k];
+    }
+    finish<T>(a, q, p, e, a.bias ? load8(a.bias + p) : Eight{});
+}
+
+// g = dy act'(z) and the sums of its columns: a workgroup takes 64 rows x 512 columns (lane: eight
+// columns, wavefront: sixteen rows, four on the way at a time), column sums in fp32 before g is rounded,
+// one partial row per 64 rows.
 constexpr int kGradRows = 64;
 template <class T, int ACT>
-__global__ __launch_bounds__(256) void act_grad_kernel(const void *dy, int64_t lddy, const void *z, int64_t ldz,
-                                                       int m, int n, void *g, float *psum)
+__global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64_t lddy, const uint16_t *z,
+                                                       int64_t ldz, int m, int n, uint16_t *g, float *psum)
 {
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-    const int c = (blockIdx.x * kWave + lane) * 4, r0 = blockIdx.y * kGradRows;
-    __shared__ f32x4 red[4][kWave];
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    const int c = (blockIdx.x * kWave + lane) * 8, r0 = blockIdx.y * kGradRows + w * (kGradRows / 4);
+    const int r1 = min(r0 + kGradRows / 4, m);
+    __shared__ float red[4][8][kWave];
+    Eight s = {};
     if (c < n)
-        for (int r = r0 + w; r < min(r0 + kGradRows, m); r += 4) {
-            const u32x2 d = *(const u32x2 *)((const uint16_t *)dy + r * lddy + c);
-            f32x4 v = {T::lo(d[0]), T::hi(d[0]), T::lo(d[1]), T::hi(d[1])};
-            if (ACT) {
-                const u32x2 e = *(const u32x2 *)((const uint16_t *)z + r * ldz + c);
-                const f32x4 t = {T::lo(e[0]), T::hi(e[0]), T::lo(e[1]), T::hi(e[1])};
+        for (int r = r0; r < r1; r += 4) {
+            u32x4 d[4], e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[i] *= activation_grad<ACT>(t[i]);
-                *(u32x2 *)((uint16_t *)g + (size_t)r * n + c) = u32x2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+            for (int u = 0; u < 4; ++u) {
+                const int64_t row = min(r + u, r1 - 1);
+                d[u] = *(const u32x4 *)(dy + row * lddy + c);
+                if (ACT)
+                    e[u] = *(const u32x4 *)(z + row * ldz + c);
             }
-            s += v;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (r + u >= r1)
+                    break;
+                Eight v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v.v[2 * i] = T::lo(d[u][i]);
+                    v.v[2 * i + 1] = T::hi(d[u][i]);
+                    if (ACT) {
+                        v.v[2 * i] *= activation_grad<ACT>(T::lo(e[u][i]));
+                        v.v[2 * i + 1] *= activation_grad<ACT>(T::hi(e[u][i]));
+                    }
+                }
+                if (ACT)
+                    *(u32x4 *)(g + (int64_t)(r + u) * n + c) = round8<T>(v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s.v[i] += v.v[i];
+            }
         }
     if (!psum)
         return;
-    red[w][lane] = s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        red[w][i][lane] = s.v[i];
     __syncthreads();
-    if (w == 0 && c < n)
-        *(f32x4 *)(psum + (size_t)blockIdx.y * n + c) = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+#pragma unroll
+    for (int i = threadIdx.x / kWave; i < 8; i += 4)
+        if (c < n)
+            psum[(size_t)blockIdx.y * n + c + i] = (red[0][i][lane] + red[1][i][lane]) + (red[2][i][lane] + red[3][i][lane]);
 }
 
-// out[c] = sum over rows of in[rows][n]: a workgroup per 64 columns, its wavefronts take every
-// fourth row.
-__global__ __launch_bounds__(256) void column_sum_kernel(const float *in, int rows, int n, float *out)
+// out[c] = sum over rows of in[rows][n]: a workgroup per 64 columns, its sixteen wavefronts take every
+// sixteenth row.
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float *in, int rows, int n, float *out)
 {
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
-    __shared__ float red[4][kWave];
+    __shared__ float red[16][kWave];
     float s = 0.f;
-    if (c < n)
-        for (int r = w; r < rows; r += 4)
+    if (c < n) {
+#pragma unroll 4
+        for (int r = w; r < rows; r += 16)
             s += in[(size_t)r * n + c];
+    }
     red[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < n)
-        out[c] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    if (w == 0 && c < n) {
+#pragma unroll
+        for (int v = 1; v < 16; ++v)
+            s += red[v][lane];
+        out[c] = s;
+    }
 }
 
 constexpr int kCUs = 256;
 
-int splits_for(int np, int nq, int nc, int tile)
+// Tile and split of a contraction.
+enum { ROWS16, ROWS32, TILE256, TILE128, TILE128_PAIR };
+struct Plan {
+    int form, splits, steps; // steps per split
+};
+
+Plan plan_product(int np, int nq, int nc, bool along)
 {
-    const int64_t tiles = std::max<int64_t>(1, (int64_t)((np + tile - 1) / tile) * ((nq + tile - 1) / tile));
     const int steps = (nc + kStep - 1) / kStep;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / tiles, steps / 8));
+    // Few rows: one launch without parts, as long as the operand is small enough for latency to count
+    // (m x n x k, rows / tiles in us: 1 x 4096 x 1024 4.0 / 9.3, 16 x 4096 x 4096 9.8 / 13.5, 16 x 1024 x 8192
+    // 16.2 / 13.5, 1 x 65536 x 1024 32.5 / 24.1, 32 x 4096 x 2048 8.1 / 12.1, 32 x 8192 x 8192 45 / 26).
+    const int64_t weights = (int64_t)np * nc;
+    if (along && nq <= 16 && weights <= 1 << 24 && nc <= 6144)
+        return {ROWS16, 1, steps};
+    if (along && nq <= 32 && weights <= 1 << 23 && nc <= 4096)
+        return {ROWS32, 1, steps};
+    const int64_t t256 = (int64_t)((np + 255) / 256) * ((nq + 255) / 256);
+    const int64_t t128 = (int64_t)((np + 127) / 128) * ((nq + 127) / 128);
+    // Time of a step over all tiles in us, by what was measured: a 256 x 256 tile 1.5 (one workgroup per
+    // CU), a 128 x 128 tile 0.49 alone on a CU with its four buffers, two of them with two buffers each
+    // 1.0.
+    const double big = 1.5 * (double)((t256 + kCUs - 1) / kCUs), one = 0.49 * (double)((t128 + kCUs - 1) / kCUs),
+                 pair = std::max(1.0, (double)t128 / (2 * kCUs) + 0.3);
+    Plan p = {TILE256, 1, steps};
+    if (one <= big && one <= pair) {
+        p.form = TILE128;
+        // idle CUs take parts of the contraction, no shorter than 16 steps: adding the parts up costs a
+        // launch and their traffic (128 x 4096 x 4096: 28.8 us in one, 16.9 in four, 19.5 in eight)
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / std::max<int64_t>(t128, 1), steps / 16));
+        p.steps = std::max(1, (steps + p.splits - 1) / p.splits);
+        p.splits = std::max(1, (steps + p.steps - 1) / p.steps);
+    } else if (pair < big)
+        p.form = TILE128_PAIR;
+    return p;
 }
 
 template <class T, bool PX, bool QX>
 hipError_t launch_product(Product a, float *scratch, hipStream_t st)
 {
-    const bool big = ((a.np + 255) / 256) * ((a.nq + 255) / 256) >= 200;
-    const int TILE = big ? 256 : 128;
-    const int splits = splits_for(a.np, a.nq, a.nc, TILE);
-    const int steps = (a.nc + kStep - 1) / kStep;
-    a.steps = (steps + splits - 1) / splits;
-    const int used = std::max(1, (steps + a.steps - 1) / std::max(a.steps, 1));
-    a.partial = used > 1 ? scratch : nullptr;
-    const dim3 grid(((a.np + TILE - 1) / TILE) * ((a.nq + TILE - 1) / TILE), used);
-    if (big)
-        product_kernel<T, PX, QX, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-    else
-        product_kernel<T, PX, QX, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
-    if (used > 1) {
+    const Plan p = plan_product(a.np, a.nq, a.nc, !PX && !QX);
+    a.steps = p.steps;
+    a.partial = p.splits > 1 ? scratch : nullptr;
+    const int tile = p.form == TILE256 ? 256 : 128;
+    const dim3 grid(((a.np + tile - 1) / tile) * ((a.nq + tile - 1) / tile), p.splits);
+    switch (p.form) {
+    case ROWS16:
+        product_rows_kernel<T, 1><<<(a.np + 15) / 16, 512, 0, st>>>(a);
+        break;
+    case ROWS32:
+        product_rows_kernel<T, 2><<<(a.np + 15) / 16, 512, 0, st>>>(a);
+        break;
+    case TILE256:
+        product_kernel<T, PX, QX, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+        break;
+    case TILE128:
+        product_kernel<T, PX, QX, 128, 128, 2, 4, 4><<<grid, 512, 0, st>>>(a);
+        break;
+    default:
+        product_kernel<T, PX, QX, 128, 128, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+    }
+    if (p.splits > 1) {
         const size_t units = (size_t)a.nq * (a.np / 8);
-        product_finish_kernel<T><<<(unsigned)std::min<size_t>((units + 255) / 256, 4096), 256, 0, st>>>(a, used);
+        product_finish_kernel<T><<<(unsigned)std::min<size_t>((units + 255) / 256, 4096), 256, 0, st>>>(a, p.splits);
     }
     return hipGetLastError();
 }
 
-size_t product_scratch(int np, int nq, int nc)
+size_t product_scratch(int np, int nq, int nc, bool along)
 {
-    const int s = splits_for(np, nq, nc, 128);
+    const int s = plan_product(np, nq, nc, along).splits;
     return s > 1 ? (size_t)s * np * nq * 4 : 0;
 }
 
@@ -447,7 +573,7 @@ BackwardScratch backward_layout(const dnnseq_linear_desc &d)
     s.g = 0;
     s.psum = d.activation ? align((size_t)d.m * d.n * 2) : 0;
     s.product = s.psum + align((size_t)((d.m + kGradRows - 1) / kGradRows) * d.n * 4);
-    s.total = s.product + std::max(product_scratch(d.k, d.m, d.n), product_scratch(d.k, d.n, d.m));
+    s.total = s.product + std::max(product_scratch(d.k, d.m, d.n, false), product_scratch(d.k, d.n, d.m, false));
     return s;
 }
 
@@ -461,9 +587,10 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
     int64_t ldg = d.lddy;
     const int parts = (d.m + kGradRows - 1) / kGradRows;
     if ((d.activation || db) && d.m) {
-        const dim3 grid((d.n + 255) / 256, parts);
+        const dim3 grid((d.n + 511) / 512, parts);
         float *psum = db ? (float *)(ws + l.psum) : nullptr;
-        const auto grad = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(dy, d.lddy, z, d.ldz, d.m, d.n, ws + l.g, psum); };
+        const auto grad = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>((const uint16_t *)dy, d.lddy, (const uint16_t *)z, d.ldz, d.m, d.n,
+                                        (uint16_t *)(ws + l.g), psum); };
         switch (d.activation) {
         case DNNSEQ_ACT_RELU:
             grad(act_grad_kernel<T, DNNSEQ_ACT_RELU>);
@@ -486,7 +613,7 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
         }
     }
     if (db)
-        column_sum_kernel<<<(d.n + kWave - 1) / kWave, 256, 0, st>>>((const float *)(ws + l.psum), parts, d.n, db);
+        column_sum_kernel<<<(d.n + kWave - 1) / kWave, 1024, 0, st>>>((const float *)(ws + l.psum), parts, d.n, db);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && dx && d.m) {
         Product a = {};
@@ -509,7 +636,7 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
 
 } // namespace
 
-size_t linear_forward_scratch(const dnnseq_linear_desc &d) { return product_scratch(d.n, d.m, d.k); }
+size_t linear_forward_scratch(const dnnseq_linear_desc &d) { return product_scratch(d.n, d.m, d.k, true); }
 size_t linear_backward_scratch(const dnnseq_linear_desc &d) { return backward_layout(d).total; }
 
 hipError_t launch_linear_forward(const dnnseq_linear_desc &d, const void *x, const void *w, const float *bias,
