@@ -24,6 +24,7 @@ constexpr int kStep = 64; // elements of the contraction per step
 
 template <bool ACROSS, int TILE>
 struct Tile {
+    static_assert(!ACROSS || TILE >= 128, "the permutation takes eight unit pairs to a row");
     static constexpr int kRows = ACROSS ? kStep : TILE;
     static constexpr int kUnits = ACROSS ? TILE / 8 : kStep / 8; // 16-byte units per row
     static constexpr int kBytes = TILE * kStep * 2;

@@ -221,7 +221,6 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
     typedef Tile<PX, TP> LP;
     typedef Tile<QX, TQ> LQ;
     constexpr int BUF = LP::kBytes + LQ::kBytes;
-    static_assert((NBUF & (NBUF - 1)) == 0 || NBUF == 3, "buffers");
     __shared__ __attribute__((aligned(256))) char lds[NBUF * BUF]; // [NBUF][P tile, Q tile]
     const uint32_t np = (a.np + TP - 1) / TP, nq = (a.nq + TQ - 1) / TQ;
     uint32_t tp, tq;
@@ -476,22 +475,32 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float *in, int r
 constexpr int kCUs = 256;
 
 // Tile and split of a contraction.
-enum { ROWS16, ROWS32, TILE256, TILE128, TILE128_PAIR };
+enum { ROWS16, ROWS32, TILE256, TILE128, TILE128_PAIR, TILE64 };
 struct Plan {
     int form, splits, steps; // steps per split
 };
 
-Plan plan_product(int np, int nq, int nc, bool along)
+// px, qx: the operand lies across
+Plan plan_product(int np, int nq, int nc, bool px, bool qx)
 {
     const int steps = (nc + kStep - 1) / kStep;
     // Few rows: one launch without parts, as long as the operand is small enough for latency to count
     // (m x n x k, rows / tiles in us: 1 x 4096 x 1024 4.0 / 9.3, 16 x 4096 x 4096 9.8 / 13.5, 16 x 1024 x 8192
     // 16.2 / 13.5, 1 x 65536 x 1024 32.5 / 24.1, 32 x 4096 x 2048 8.1 / 12.1, 32 x 8192 x 8192 45 / 26).
     const int64_t weights = (int64_t)np * nc;
-    if (along && nq <= 16 && weights <= 1 << 24 && nc <= 6144)
+    if (!px && !qx && nq <= 16 && weights <= 1 << 24 && nc <= 6144)
         return {ROWS16, 1, steps};
-    if (along && nq <= 32 && weights <= 1 << 23 && nc <= 4096)
+    if (!px && !qx && nq <= 32 && weights <= 1 << 23 && nc <= 4096)
         return {ROWS32, 1, steps};
+    // Up to 64 rows: six buffers of a 128 x 64 tile, 100 KB on the way to each CU (24 x 4096 x 16384 from
+    // memory: 38.4 us, 42.7 with 128 x 128)
+    if (!qx && nq <= 64) {
+        Plan p = {TILE64, 1, steps};
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / ((np + 127) / 128), steps / 16));
+        p.steps = std::max(1, (steps + p.splits - 1) / p.splits);
+        p.splits = std::max(1, (steps + p.steps - 1) / p.steps);
+        return p;
+    }
     const int64_t t256 = (int64_t)((np + 255) / 256) * ((nq + 255) / 256);
     const int64_t t128 = (int64_t)((np + 127) / 128) * ((nq + 127) / 128);
     // Time of a step over all tiles in us, by what was measured: a 256 x 256 tile 1.5 (one workgroup per
@@ -515,11 +524,12 @@ Plan plan_product(int np, int nq, int nc, bool along)
 template <class T, bool PX, bool QX>
 hipError_t launch_product(Product a, float *scratch, hipStream_t st)
 {
-    const Plan p = plan_product(a.np, a.nq, a.nc, !PX && !QX);
+    const Plan p = plan_product(a.np, a.nq, a.nc, PX, QX);
     a.steps = p.steps;
     a.partial = p.splits > 1 ? scratch : nullptr;
     const int tile = p.form == TILE256 ? 256 : 128;
-    const dim3 grid(((a.np + tile - 1) / tile) * ((a.nq + tile - 1) / tile), p.splits);
+    const int rows = p.form == TILE64 ? 64 : tile;
+    const dim3 grid(((a.np + tile - 1) / tile) * ((a.nq + rows - 1) / rows), p.splits);
     switch (p.form) {
     case ROWS16:
         product_rows_kernel<T, 1><<<(a.np + 15) / 16, 512, 0, st>>>(a);
@@ -533,6 +543,10 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
     case TILE128:
         product_kernel<T, PX, QX, 128, 128, 2, 4, 4><<<grid, 512, 0, st>>>(a);
         break;
+    case TILE64:
+        if constexpr (!QX)
+            product_kernel<T, PX, QX, 128, 64, 4, 1, 6><<<grid, 256, 0, st>>>(a);
+        break;
     default:
         product_kernel<T, PX, QX, 128, 128, 2, 4, 2><<<grid, 512, 0, st>>>(a);
     }
@@ -543,9 +557,9 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
     return hipGetLastError();
 }
 
-size_t product_scratch(int np, int nq, int nc, bool along)
+size_t product_scratch(int np, int nq, int nc, bool px, bool qx)
 {
-    const int s = plan_product(np, nq, nc, along).splits;
+    const int s = plan_product(np, nq, nc, px, qx).splits;
     return s > 1 ? (size_t)s * np * nq * 4 : 0;
 }
 
@@ -573,7 +587,7 @@ BackwardScratch backward_layout(const dnnseq_linear_desc &d)
     s.g = 0;
     s.psum = d.activation ? align((size_t)d.m * d.n * 2) : 0;
     s.product = s.psum + align((size_t)((d.m + kGradRows - 1) / kGradRows) * d.n * 4);
-    s.total = s.product + std::max(product_scratch(d.k, d.m, d.n, false), product_scratch(d.k, d.n, d.m, false));
+    s.total = s.product + std::max(product_scratch(d.k, d.m, d.n, true, false), product_scratch(d.k, d.n, d.m, true, true));
     return s;
 }
 
@@ -636,7 +650,7 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
 
 } // namespace
 
-size_t linear_forward_scratch(const dnnseq_linear_desc &d) { return product_scratch(d.n, d.m, d.k, true); }
+size_t linear_forward_scratch(const dnnseq_linear_desc &d) { return product_scratch(d.n, d.m, d.k, false, false); }
 size_t linear_backward_scratch(const dnnseq_linear_desc &d) { return backward_layout(d).total; }
 
 hipError_t launch_linear_forward(const dnnseq_linear_desc &d, const void *x, const void *w, const float *bias,
