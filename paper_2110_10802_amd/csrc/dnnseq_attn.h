@@ -7,10 +7,10 @@
 //   along   its rows are matrix rows, the dimension is contracted: 16 consecutive bytes per lane
 //   across  its rows are contracted, the dimension gives the matrix rows: two transposing reads
 // A product whose result has (tile row, own row) as (matrix row, column) leaves lane l = 32 h + c with
-// the rows 8 (r/4) + 4 h + r % 4 of column c in register r.  Registers 8 m .. 8 m + 7, packed, are the
-// column operand of a product that contracts rows 16 m .. 16 m + 15, with the rows in the order
-// 4 h + {0..3}, 8 + 4 h + {0..3}: the across reads use the same order, so probabilities and score
-// gradients go from one product into the next without leaving their lane.
+// the rows 8 (r/4) + 4 h + r % 4 of column c in register r.  Registers 4 m .. 4 m + 3 and 8 + 4 m .. of it,
+// packed, are the column operand of a product that contracts the rows 8 m + 4 h + {0..3} and
+// 16 + 8 m + 4 h + {0..3}: the across reads use the same order, so probabilities and score gradients go
+// from one product into the next without leaving their lane.
 #pragma once
 #include "dnnseq_dev.h"
 
@@ -19,11 +19,13 @@ namespace dsq {
 constexpr int kTileRows = 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// The 16-byte unit of row `row` at which unit u is kept: both kinds of reads meet 64 banks evenly.
+// Unit u of row `row` is kept at u ^ this: 16 consecutive rows read along, and four rows of four units
+// read across, meet the 64 banks evenly (no conflicts counted; 4 cycles more per read along without the
+// row's third bit).
 template <int RS>
 __device__ __forceinline__ int unit_swizzle(int row)
 {
-    return RS == 128 ? (row & 3) << 2 | (row >> 2 & 1) : (row >> 1 & 1) << 2 | (row >> 2 & 1);
+    return RS == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 1) | (row >> 3 & 1) << 1;
 }
 
 // Loads of tiles of one tensor (one head of one request).
@@ -75,7 +77,7 @@ struct AlongReader {
     }
 };
 
-// Contracted rows 16 m .. 16 m + 15 in the order above, elements 32 e .. 32 e + 31.
+// Half m % 2 of the contracted rows 32 (m/2) .. + 31, in the order above; elements 32 e .. 32 e + 31.
 template <int RS>
 struct AcrossReader {
     uint32_t off, flip;
@@ -87,10 +89,20 @@ struct AcrossReader {
     }
     __device__ __forceinline__ u32x4 get(const char *lds, int m, int e) const
     {
-        const char *p = lds + off + (flip ^ (e * 64)) + m * (16 * RS * 2);
-        return join(read_tr((const uint16_t *)p), read_tr((const uint16_t *)(p + 8 * RS * 2)));
+        // (eight rows on, the permutation has unit bit 1 the other way; sixteen on, it is the same)
+        const char *p = lds + off + (flip ^ (e * 64 | m % 2 * 32)) + m / 2 * (32 * RS * 2) + m % 2 * (8 * RS * 2);
+        return join(read_tr((const uint16_t *)p), read_tr((const uint16_t *)(p + 16 * RS * 2)));
     }
 };
+// Register r of a result belongs to the column operand of half half_of(r), its pair pair_of(r).
+constexpr int half_of(int r) { return r / 4 % 2; }
+constexpr int pair_of(int r) { return r / 8 * 2 + r % 4 / 2; }
+template <class T>
+__device__ __forceinline__ u32x4 pack_half(const f32x16 &s, int h)
+{
+    return u32x4{T::pack(s[4 * h], s[4 * h + 1]), T::pack(s[4 * h + 2], s[4 * h + 3]),
+                 T::pack(s[8 + 4 * h], s[8 + 4 * h + 1]), T::pack(s[8 + 4 * h + 2], s[8 + 4 * h + 3])};
+}
 
 // A lane's own row as a column operand: elements 16 s + 8 (lane / 32) .. + 7; zeros outside.
 __device__ __forceinline__ u32x4 own_fragment(const uint16_t *row, bool inside, int dim, int s)

@@ -94,10 +94,8 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            u32x4 p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) // rounded to the operands' type: p is at most 2^8, its error 2^-8 or 2^-11 of it
-                p[i] = T::pack(s[b][8 * h + 2 * i], s[b][8 * h + 2 * i + 1]);
+            // rounded to the operands' type: p is at most 2^8, its error 2^-8 or 2^-11 of it
+            const u32x4 p = pack_half<T>(s[b], h);
 #pragma unroll
             for (int e = 0; e < NS; ++e)
                 acc[e] = T::mma32(across.get(vt, 2 * b + h, e), p, acc[e]);

@@ -4,12 +4,13 @@
 // Two passes, each with one owner for every output element, so nothing is added atomically: seven
 // products instead of the five of a single pass.
 //
-//   attn_delta  delta of every row (and, for fp16, the factor that keeps ds in range)
-//   attn_dkv    128 keys per workgroup, 32 per wavefront (columns of s = q k^T): walks the query rows
-//               of the key head's group in tiles of 64; p and ds come out as the column operands of
-//               dv^T += dout^T p and dk^T += q^T ds
+//   attn_delta  delta of every row from the rounded o, lse in base 2 (and, for fp16, the factor that
+//               keeps ds in range)
 //   attn_dq     128 rows per workgroup, 32 per wavefront (columns of s^T = k q^T): walks the keys;
 //               ds^T is the column operand of dq^T += k^T ds^T
+//   attn_dkv    128 keys per workgroup, 32 per wavefront (columns of s = q k^T): walks the query rows of
+//               the key head's group; p and ds come out as the column operands of dv^T += dout^T p and
+//               dk^T += q^T ds
 //
 // fp16: ds has entries of the size of dp / keys, which fp16 may not hold.  All of them are multiplied
 // by one power of two c, taken from max |dout_i| max |v_j| >= max |dp|, and dq and dk divided by it.
@@ -29,7 +30,8 @@ struct Backward {
     dnnseq_stride sq, sk, sv, so, sdo, sdq, sdk, sdv;
     int batch, q_heads, kv_heads, group, q_len, kv_len, dim, causal;
     float scale, scale2;
-    float *delta;    // [batch][q_heads][q_len]
+    float *minus, *lse2; // [batch][q_heads][q_pad]; -delta; lse2: base 2, +infinity where a row sees nothing (p = 0)
+    int q_pad;           // q_len to a whole number of tiles
     float *bound;    // fp16: [bounds] squares of row norms, their maxima per workgroup (dout, then v)
     int bounds_q, bounds_v;
     int head_splits; // workgroups that share the heads of a group in attn_dkv
@@ -41,42 +43,57 @@ __device__ __forceinline__ int64_t row_offset(const dnnseq_stride &s, int b, int
     return b * s.batch + head * s.head + token * s.token;
 }
 
-// 16 lanes to a row; rows of dout first (delta and norm), then, for fp16, rows of v (norm).
+// A workgroup per 64 rows, 16 lanes to a row; rows of dout first (delta and norm), then, for fp16, rows of
+// v (norm).
 template <class T>
 __global__ __launch_bounds__(256) void attn_delta_kernel(Backward a)
 {
     const int lane = threadIdx.x % 16, c = lane * 8;
     const bool of_v = (int)blockIdx.x >= a.bounds_q;
-    const size_t row = (size_t)(blockIdx.x - (of_v ? a.bounds_q : 0)) * 16 + threadIdx.x / 16;
     const int len = of_v ? a.kv_len : a.q_len, heads = of_v ? a.kv_heads : a.q_heads;
-    float dot = 0.f, norm = 0.f;
-    const bool in = row < (size_t)a.batch * heads * len;
-    if (in) {
-        const int t = row % len, h = row / len % heads, b = row / len / heads;
-        const int top = of_v ? clamp_len(a.kv_lens, b, len) : clamp_len(a.q_lens, b, len);
-        if (t < top && c < a.dim) {
-            const u32x4 x = *(const u32x4 *)((of_v ? a.v + row_offset(a.sv, b, h, t) : a.dout + row_offset(a.sdo, b, h, t)) + c);
-            const u32x4 y = of_v ? x : *(const u32x4 *)(a.o + row_offset(a.so, b, h, t) + c);
+    const int item = blockIdx.x - (of_v ? a.bounds_q : 0), tiles = (len + kTileRows - 1) / kTileRows;
+    const int bh = item / tiles, t0 = item % tiles * kTileRows + threadIdx.x / 16, h = bh % heads, b = bh / heads;
+    const int top = clamp_len(of_v ? a.kv_lens : a.q_lens, b, len);
+    u32x4 x[4], y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                dot += T::lo(x[i]) * T::lo(y[i]) + T::hi(x[i]) * T::hi(y[i]);
-                norm += T::lo(x[i]) * T::lo(x[i]) + T::hi(x[i]) * T::hi(x[i]);
-            }
+    for (int i = 0; i < 4; ++i) {
+        const int t = t0 + 16 * i;
+        x[i] = y[i] = u32x4{0, 0, 0, 0};
+        if (t < top && c < a.dim) {
+            x[i] = *(const u32x4 *)((of_v ? a.v + row_offset(a.sv, b, h, t) : a.dout + row_offset(a.sdo, b, h, t)) + c);
+            if (!of_v)
+                y[i] = *(const u32x4 *)(a.o + row_offset(a.so, b, h, t) + c);
         }
     }
-    dot = mbk::row16_sum(dot);
-    if (in && !of_v && lane == 0)
-        a.delta[row] = dot;
+    float largest = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float dot = 0.f, norm = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            dot += T::lo(x[i][j]) * T::lo(y[i][j]) + T::hi(x[i][j]) * T::hi(y[i][j]);
+            norm += T::lo(x[i][j]) * T::lo(x[i][j]) + T::hi(x[i][j]) * T::hi(x[i][j]);
+        }
+        dot = mbk::row16_sum(dot);
+        const int t = t0 + 16 * i;
+        if (!of_v && lane == 0) {
+            const size_t at = (size_t)bh * a.q_pad + t;
+            const float l = t < top ? a.lse[(size_t)bh * len + t] : -INFINITY;
+            a.minus[at] = -dot;
+            a.lse2[at] = l == -INFINITY ? INFINITY : l * kLog2e;
+        }
+        if (T::kHalf)
+            largest = fmaxf(largest, mbk::row16_sum(norm));
+    }
     if (T::kHalf) {
-        norm = mbk::row16_sum(norm);
         __shared__ float red[16];
         if (lane == 0)
-            red[threadIdx.x / 16] = norm;
+            red[threadIdx.x / 16] = largest;
         __syncthreads();
         if (threadIdx.x == 0) {
             for (int i = 1; i < 16; ++i)
-                norm = fmaxf(norm, red[i]);
-            a.bound[blockIdx.x] = norm;
+                largest = fmaxf(largest, red[i]);
+            a.bound[blockIdx.x] = largest;
         }
     }
 }
@@ -115,16 +132,6 @@ __device__ __forceinline__ float range_factor(const Backward &a)
     return ldexpf(1.0f, min(max(e, -100), 100));
 }
 
-template <class T>
-__device__ __forceinline__ u32x4 pack8(const f32x16 &s, int h)
-{
-    u32x4 p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        p[i] = T::pack(s[8 * h + 2 * i], s[8 * h + 2 * i + 1]);
-    return p;
-}
-
 // Four consecutive elements of a transposed result (register 4 i .. 4 i + 3 of block e).
 template <class T, int NS>
 __device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[NS], int dim, float f)
@@ -156,67 +163,36 @@ __device__ __forceinline__ void store_part(float *row, const f32x16 (&acc)[NS], 
 }
 
 // ---- dk, dv --------------------------------------------------------------------------------------
-// A tile of 64 query rows for 32 keys.  Row t sees keys up to t + shift.
-template <class T, int NS, int RS, bool MASK>
-__device__ __forceinline__ void dkv_tile(const char *__restrict__ qt, const char *__restrict__ dt,
-                                         const float *__restrict__ lse2, const float *__restrict__ delta,
-                                         const AlongReader<RS> &along, const AcrossReader<RS> &across,
-                                         const u32x4 (&k)[2 * NS], const u32x4 (&v)[2 * NS], f32x16 (&dk)[NS],
-                                         f32x16 (&dv)[NS], int t0, int key, int shift, float scale2, float c)
+// 64 floats into LDS by one wavefront.
+__device__ __forceinline__ void load_floats(const float *p, char *lds)
 {
-    const int half = threadIdx.x % kWave / 32;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i)
-            s = T::mma32(along.get(qt, b, i), k[i], s);
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i)
-            dp = T::mma32(along.get(dt, b, i), v[i], dp);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r0 = 32 * b + 8 * i + 4 * half;
-            const f32x4 ls = *(const f32x4 *)(lse2 + r0), de = *(const f32x4 *)(delta + r0);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float p = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], scale2, -ls[j]));
-                if (MASK)
-                    p = key <= t0 + r0 + j + shift ? p : 0.f;
-                s[4 * i + j] = p;
-                dp[4 * i + j] = p * (dp[4 * i + j] - de[j]) * c;
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) { // p and ds are rounded to the operands' type
-            const u32x4 p = pack8<T>(s, h);
-#pragma unroll
-            for (int e = 0; e < NS; ++e)
-                dv[e] = T::mma32(across.get(dt, 2 * b + h, e), p, dv[e]);
-            const u32x4 ds = pack8<T>(dp, h);
-#pragma unroll
-            for (int e = 0; e < NS; ++e)
-                dk[e] = T::mma32(across.get(qt, 2 * b + h, e), ds, dk[e]);
-        }
-    }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer(p, kTileRows * 4), (lds_void *)lds, 4, threadIdx.x % kWave * 4, 0,
+                                             0, 0);
 }
 
-template <class T, int NS>
+// A wavefront has the accumulators, keys and values of its 32 keys in registers (at 128 elements one
+// wavefront to a SIMD), so its own instructions have to overlap: blocks of 32 rows are pipelined.  In one
+// phase the matrix cores take the scores of the next block while the vector units turn the second half
+// of this one's into p and ds, in the other this block's p and ds while the vector units take the first
+// half of the next one's; each phase reads the other's operands from LDS.  Three buffers: a tile is read
+// first one step before its own.  2 x 16 heads x 4093 x 128, causal: 474 us with the phases one after the
+// other, 321 with all of p and ds in one phase.
+template <class T, int NS, bool CAUSAL>
 __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward a)
 {
     constexpr int RS = NS > 2 ? 128 : 64, KEYS = 128;
     typedef TileLoader<RS, 256> Load;
-    constexpr int BUF = 2 * Load::kBytes + 2 * kTileRows * 4;
-    __shared__ __attribute__((aligned(256))) char lds[2 * BUF]; // [2][q, dout, lse, delta]
+    constexpr int LSE = 2 * Load::kBytes, DELTA = LSE + kTileRows * 4, BUF = DELTA + kTileRows * 4;
+    __shared__ __attribute__((aligned(256))) char lds[3 * BUF]; // [3][q, dout, lse2, delta]
     const int tiles = (a.kv_len + KEYS - 1) / KEYS;
     const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
     const int hs = item % a.head_splits, tile = item / a.head_splits % tiles, unit = item / a.head_splits / tiles;
     const int b = unit / a.kv_heads, g = unit % a.kv_heads;
     const int key0 = tile * KEYS; // (the first keys are seen by most rows: they come first)
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
-    const int lane = threadIdx.x % kWave, w = wave_id();
+    const int lane = threadIdx.x % kWave, w = wave_id(), half = lane / 32;
     const int key = key0 + w * 32 + lane % 32, shift = kl - ql;
-    const float c = range_factor<T>(a);
+    const float c = range_factor<T>(a), scale2 = a.scale2;
 
     u32x4 k[2 * NS], v[2 * NS];
     const uint16_t *krow = a.k + row_offset(a.sk, b, g, key), *vrow = a.v + row_offset(a.sv, b, g, key);
@@ -235,47 +211,172 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward 
         dk[e] = dv[e] = f32x16{};
 
     // rows that see any key of the workgroup: t >= key0 - shift, in whole tiles
-    const int t_first = a.causal ? max(0, key0 - shift) / kTileRows * kTileRows : 0;
+    const int t_first = CAUSAL ? max(0, key0 - shift) / kTileRows * kTileRows : 0;
+    const int h0 = g * a.group + a.group * hs / a.head_splits, h1 = g * a.group + a.group * (hs + 1) / a.head_splits;
     const int per_head = key0 < kl && ql > t_first ? (ql - t_first + kTileRows - 1) / kTileRows : 0;
-    const int h0 = a.group * hs / a.head_splits, h1 = a.group * (hs + 1) / a.head_splits;
+    const int steps = per_head * (h1 - h0);
     Load lq, ld;
-    const auto issue = [&](int step, char *buf) __attribute__((always_inline)) {
-        const int h = g * a.group + h0 + step / per_head, t0 = t_first + step % per_head * kTileRows;
-        lq.base = (const char *)(a.q + row_offset(a.sq, b, h, 0));
-        ld.base = (const char *)(a.dout + row_offset(a.sdo, b, h, 0));
-        lq.load(buf, t0, ql);
-        ld.load(buf + Load::kBytes, t0, ql);
-        // lse (base 2; +infinity where a row sees nothing: p = 0) and delta of 64 rows
-        if (w == 0) {
-            const size_t at = ((size_t)b * a.q_heads + h) * a.q_len;
-            const int t = t0 + lane;
-            const float l = t < ql ? a.lse[at + t] : -INFINITY;
-            float *f = (float *)(buf + 2 * Load::kBytes);
-            f[lane] = l == -INFINITY ? INFINITY : l * kLog2e;
-            f[kTileRows + lane] = t < ql ? a.delta[at + t] : 0.f;
-        }
-    };
     lq.init(a.q, a.sq.token, a.dim);
     ld.init(a.dout, a.sdo.token, a.dim);
-    const int steps = per_head * (h1 - h0);
-    if (steps)
-        issue(0, lds);
-    for (int n = 0; n < steps; ++n) {
-        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
-        __syncthreads();                    // and everyone's; the other buffer is no longer read
-        const auto step = [&](const char *__restrict__ cur, char *__restrict__ nxt) __attribute__((always_inline)) {
-            if (n + 1 < steps)
-                issue(n + 1, nxt);
-            const float *f = (const float *)(cur + 2 * Load::kBytes);
-            const int t0 = t_first + n % per_head * kTileRows, w0 = key0 + w * 32;
-            if (!a.causal || w0 + 31 <= t0 + shift)
-                dkv_tile<T, NS, RS, false>(cur, cur + Load::kBytes, f, f + kTileRows, along, across, k, v, dk, dv, t0,
-                                           key, shift, a.scale2, c);
-            else if (w0 <= t0 + kTileRows - 1 + shift)
-                dkv_tile<T, NS, RS, true>(cur, cur + Load::kBytes, f, f + kTileRows, along, across, k, v, dk, dv, t0,
-                                          key, shift, a.scale2, c);
-        };
-        step(lds + (n & 1) * BUF, lds + (~n & 1) * BUF);
+    // Head and first row of the tile that is requested next, and where it lies.  The rows are walked from
+    // the last: the workgroups of a head, which start at different rows where `causal`, then read the same
+    // tiles at the same time and find them in their XCD's L2 (315 us for 2 x 16 heads x 4093 x 128 from
+    // the first row on: q and dout of four heads are 8 MB, and came from beyond it at 3.5 TB/s).
+    const int t_last = t_first + (per_head - 1) * kTileRows;
+    int nh = h0, nt = t_last;
+    const float *rows2 = nullptr, *rows1 = nullptr;
+    const auto seek = [&] __attribute__((always_inline)) {
+        const size_t at = ((size_t)b * a.q_heads + nh) * a.q_pad + nt;
+        rows2 = a.lse2 + at;
+        rows1 = a.minus + at;
+        lq.base = (const char *)(a.q + row_offset(a.sq, b, nh, nt));
+        ld.base = (const char *)(a.dout + row_offset(a.sdo, b, nh, nt));
+    };
+    const auto issue = [&](char *__restrict__ buf) __attribute__((always_inline)) {
+        lq.load(buf, 0, ql - nt);
+        ld.load(buf + Load::kBytes, 0, ql - nt);
+        load_floats(w % 2 ? rows1 : rows2, buf + (w % 2 ? DELTA : LSE)); // (twice each: no branch)
+        nt -= kTileRows;
+        rows2 -= kTileRows;
+        rows1 -= kTileRows;
+        lq.base -= (int64_t)kTileRows * lq.pitch;
+        ld.base -= (int64_t)kTileRows * ld.pitch;
+        if (nt < t_first) {
+            nt = t_last;
+            nh = min(nh + 1, h1 - 1); // (past the last tile: that head again, never used)
+            seek();
+        }
+    };
+    f32x16 s[2], dp[2];
+    u32x4 fq[2 * NS], fd[2 * NS], xq[2][NS], xd[2][NS]; // operands: along for scores, across for sums
+    // lse2 and -delta of rows 8 i + 4 half .. of a block, i = i0 and i0 + 2
+    f32x4 ls[4];
+    f32x16 de;
+    const auto read_lse = [&](const char *__restrict__ buf, int block, int i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = i0; i < 4; i += 2)
+            ls[i] = *(const f32x4 *)(buf + LSE + (32 * block + 8 * i + 4 * half) * 4);
+    };
+    const auto read_delta = [&](const char *__restrict__ buf, int block) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = *(const f32x4 *)(buf + DELTA + (32 * block + 8 * i + 4 * half) * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                de[4 * i + j] = v[j];
+        }
+    };
+    u32x4 p[2], ds[2]; // rounded to the operands' type
+    // Element n of a block's p and ds, those of p[0] and ds[0] first; with the odd ones a pair is packed.
+    const auto weight = [&](int block, int n, int t0) __attribute__((always_inline)) {
+        const int r = n % 8 / 4 * 8 + n / 8 * 4 + n % 4;
+        float w1 = __builtin_amdgcn_exp2f(fmaf(s[block][r], scale2, -ls[r / 4][r % 4]));
+        if (CAUSAL) // row t sees keys up to t + shift
+            w1 = key - shift - t0 - 4 * half <= 32 * block + 8 * (r / 4) + r % 4 ? w1 : 0.f;
+        s[block][r] = w1;
+        dp[block][r] *= w1;
+        if (T::kHalf)
+            dp[block][r] *= c;
+        if (n % 2) {
+            p[half_of(r)][pair_of(r)] = T::pack(s[block][r - 1], s[block][r]);
+            ds[half_of(r)][pair_of(r)] = T::pack(dp[block][r - 1], dp[block][r]);
+        }
+    };
+    // Operand j of 4 NS: along for the scores, across for the sums.
+    const auto read_along = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
+        (j % 2 ? fd : fq)[j / 2] = along.get(buf + j % 2 * Load::kBytes, block, j / 2);
+    };
+    const auto read_across = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
+        const int h = j / (2 * NS), e = j / 2 % NS;
+        (j % 2 ? xq : xd)[h][e] = across.get(buf + (1 - j % 2) * Load::kBytes, 2 * block + h, e);
+    };
+    const auto score = [&](int block, int j) __attribute__((always_inline)) {
+        if (j % 2)
+            dp[block] = T::mma32(fd[j / 2], v[j / 2], j == 1 ? de : dp[block]); // dp - delta
+        else
+            s[block] = T::mma32(fq[j / 2], k[j / 2], j == 0 ? f32x16{} : s[block]);
+    };
+    const auto sum = [&](int j) __attribute__((always_inline)) {
+        const int h = j / (2 * NS), e = j / 2 % NS;
+        if (j % 2)
+            dk[e] = T::mma32(xq[h][e], ds[h], dk[e]);
+        else
+            dv[e] = T::mma32(xd[h][e], p[h], dv[e]);
+    };
+    const auto landed = [] __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const auto step = [&](const char *__restrict__ cur, const char *__restrict__ nxt, char *__restrict__ spare, int t0,
+                          int t1) __attribute__((always_inline)) {
+        issue(spare);
+        // (the barriers keep the order: left to itself the compiler puts the products in a row, and the
+        // vector units wait for the last of them)
+#pragma unroll
+        for (int block = 0; block < 2; ++block) {
+#pragma unroll
+            for (int j = 0; j < 4 * NS; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                score(block ^ 1, j);
+                read_across(cur, block, j);
+                if (j == 0)
+                    read_lse(block ? nxt : cur, block ^ 1, 0);
+                if (j == 1) // (the scores of this phase have taken theirs)
+                    read_delta(nxt, block);
+#pragma unroll
+                for (int n = 8 + 8 * j / (4 * NS); n < 8 + 8 * (j + 1) / (4 * NS); ++n)
+                    weight(block, n, t0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4 * NS; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                sum(j);
+                read_along(nxt, block, j);
+                if (j == 0)
+                    read_lse(block ? nxt : cur, block ^ 1, 1);
+                if (j >= 2 * NS) // (the sums with p[0] and ds[0] are behind)
+#pragma unroll
+                    for (int n = 8 * (j - 2 * NS) / (2 * NS); n < 8 * (j + 1 - 2 * NS) / (2 * NS); ++n)
+                        weight(block ^ 1, n, block ? t1 : t0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (steps) {
+        seek();
+        issue(lds);
+        issue(lds + BUF);
+        landed();
+        read_delta(lds, 0);
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            read_along(lds, 0, j);
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            score(0, j);
+        read_delta(lds, 1);
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            read_along(lds, 1, j);
+        read_lse(lds, 0, 0);
+        read_lse(lds, 0, 1);
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+            weight(0, n, t_last);
+        uint32_t at = 0;
+        int t0 = t_last;
+        for (int n = 0; n < steps; ++n) {
+            const uint32_t nxt = at == 2 * BUF ? 0 : at + BUF, spare = nxt == 2 * BUF ? 0 : nxt + BUF;
+            // the next tile is here, and nobody reads the one before this any more
+            landed();
+            const int t1 = t0 == t_first ? t_last : t0 - kTileRows;
+            step(lds + at, lds + nxt, lds + spare, t0, t1);
+            at = nxt;
+            t0 = t1;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70); // (no load into LDS may outlive the workgroup)
     }
     if (key >= a.kv_len)
         return;
@@ -316,61 +417,30 @@ __global__ __launch_bounds__(256) void attn_dkv_sum_kernel(Backward a)
 }
 
 // ---- dq ------------------------------------------------------------------------------------------
-template <class T, int NS, int RS, bool MASK>
-__device__ __forceinline__ void dq_tile(const char *__restrict__ kt, const char *__restrict__ vt,
-                                        const AlongReader<RS> &along, const AcrossReader<RS> &across,
-                                        const u32x4 (&q)[2 * NS], const u32x4 (&d)[2 * NS], f32x16 (&dq)[NS], int key0,
-                                        int limit, float lse2, float delta, float scale2, float c)
-{
-    const int half = threadIdx.x % kWave / 32;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i)
-            s = T::mma32(along.get(kt, b, i), q[i], s);
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i)
-            dp = T::mma32(along.get(vt, b, i), d[i], dp);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float p = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2));
-            if (MASK)
-                p = key0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 < limit ? p : 0.f;
-            dp[r] = p * (dp[r] - delta) * c;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32x4 ds = pack8<T>(dp, h);
-#pragma unroll
-            for (int e = 0; e < NS; ++e)
-                dq[e] = T::mma32(across.get(kt, 2 * b + h, e), ds, dq[e]);
-        }
-    }
-}
-
+// The same pipeline over blocks of 32 keys; the wavefront's 32 query rows are the columns.  ds is kept as
+// the sum of two 16-bit values (a second product with the same operand from LDS): that leaves dq the
+// precision of its own rounding, where one rounding of ds costs as much again.  On the way the rows' sums
+// of ds give what delta lacks, o having been rounded: attn_dkv reads the sum.
 template <class T, int NS>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
+__global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dq_kernel(Backward a)
 {
     constexpr int RS = NS > 2 ? 128 : 64, ROWS = 128;
     typedef TileLoader<RS, 256> Load;
-    __shared__ __attribute__((aligned(256))) char lds[4 * Load::kBytes]; // [2][keys, values]
+    constexpr int BUF = 2 * Load::kBytes;
+    __shared__ __attribute__((aligned(256))) char lds[3 * BUF]; // [3][keys, values]
     const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
     const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
     const int unit = item / tiles, b = unit / a.kv_heads, g = unit % a.kv_heads;
-    const int r0 = (tiles - 1 - item % tiles) * ROWS;
+    const int r0 = (tiles - 1 - item % tiles) * ROWS; // the rows that see most keys first
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
-    const int lane = threadIdx.x % kWave, w = wave_id();
-    const auto limit_of = [&](int r) {
+    const int lane = threadIdx.x % kWave, w = wave_id(), half = lane / 32;
+    const auto limit_of = [&](int r) { // one past the last key that a row sees
         const int t = r / a.group;
         return r >= rows || t >= ql ? 0 : a.causal ? min(kl, t + kl - ql + 1) : kl;
     };
     const int r = r0 + w * 32 + lane % 32, limit = limit_of(r);
-    const int end = limit_of(min(r0 + ROWS, ql * a.group) - 1 >= r0 ? min(r0 + ROWS, ql * a.group) - 1 : rows);
-    const int wr = min(r0 + w * 32 + 32, ql * a.group) - 1;
-    const int wave_end = wr >= r0 + w * 32 ? limit_of(wr) : 0;
-    const int wave_free = min(limit_of(r0 + w * 32), limit_of(r0 + w * 32 + 31));
-    const float c = range_factor<T>(a);
+    const int last = min(r0 + ROWS, ql * a.group) - 1, end = last >= r0 ? limit_of(last) : 0;
+    const float c = range_factor<T>(a), scale2 = a.scale2;
 
     u32x4 q[2 * NS], d[2 * NS];
     const int head = g * a.group + r % a.group, token = r / a.group;
@@ -381,9 +451,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
         q[i] = own_fragment(qrow, in, a.dim, i);
         d[i] = own_fragment(drow, in, a.dim, i);
     }
-    const size_t ri = ((size_t)b * a.q_heads + head) * a.q_len + token;
-    const float lse = in ? a.lse[ri] : -INFINITY, delta = in ? a.delta[ri] : 0.f;
-    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    const size_t ri = ((size_t)b * a.q_heads + head) * a.q_pad + token;
+    const float lse2 = in ? a.lse2[ri] : INFINITY, minus = in ? a.minus[ri] : 0.f;
+    float rest = 0.f;
     Load lk, lv;
     lk.init(a.k + row_offset(a.sk, b, g, 0), a.sk.token, a.dim);
     lv.init(a.v + row_offset(a.sv, b, g, 0), a.sv.token, a.dim);
@@ -391,49 +461,136 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
     AcrossReader<RS> across;
     along.init();
     across.init();
-    f32x16 dq[NS];
+    f32x16 dq[NS], from; // from: -delta, where dp starts
 #pragma unroll
     for (int e = 0; e < NS; ++e)
         dq[e] = f32x16{};
-    if (0 < end) {
-        lk.load(lds, 0, kl);
-        lv.load(lds + Load::kBytes, 0, kl);
-    }
-    for (int k0 = 0, turn = 0; k0 < end; k0 += kTileRows, turn ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
-        __syncthreads();                    // and everyone's; the other buffer is no longer read
-        const auto step = [&](const char *__restrict__ cur, char *__restrict__ nxt) __attribute__((always_inline)) {
-            if (k0 + kTileRows < end) {
-                lk.load(nxt, k0 + kTileRows, kl);
-                lv.load(nxt + Load::kBytes, k0 + kTileRows, kl);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        from[i] = minus;
+    int nk = 0; // first key of the tile that is requested next
+    const auto issue = [&](char *__restrict__ buf) __attribute__((always_inline)) {
+        lk.load(buf, 0, kl - nk); // (past the end: zeros, no memory is read)
+        lv.load(buf + Load::kBytes, 0, kl - nk);
+        nk += kTileRows;
+        lk.base += (int64_t)kTileRows * lk.pitch;
+        lv.base += (int64_t)kTileRows * lv.pitch;
+    };
+    f32x16 s[2], dp[2];
+    u32x4 fk[2 * NS], fv[2 * NS], xk[2][NS], hi[2], lo[2];
+    const auto weight = [&](int block, int n, int key0) __attribute__((always_inline)) {
+        const int r = n % 8 / 4 * 8 + n / 8 * 4 + n % 4;
+        float p = __builtin_amdgcn_exp2f(fmaf(s[block][r], scale2, -lse2));
+        p = 32 * block + 8 * (r / 4) + r % 4 < limit - key0 - 4 * half ? p : 0.f;
+        dp[block][r] *= p;
+        if (T::kHalf)
+            dp[block][r] *= c;
+        rest += dp[block][r];
+        if (n % 2) {
+            const float x = dp[block][r - 1], y = dp[block][r];
+            const uint32_t v = T::pack(x, y);
+            hi[half_of(r)][pair_of(r)] = v;
+            lo[half_of(r)][pair_of(r)] = T::pack(x - T::lo(v), y - T::hi(v));
+        }
+    };
+    const auto read_along = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
+        (j % 2 ? fv : fk)[j / 2] = along.get(buf + j % 2 * Load::kBytes, block, j / 2);
+    };
+    const auto read_across = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
+        xk[j / NS][j % NS] = across.get(buf, 2 * block + j / NS, j % NS);
+    };
+    const auto score = [&](int block, int j) __attribute__((always_inline)) {
+        if (j % 2)
+            dp[block] = T::mma32(fv[j / 2], d[j / 2], j == 1 ? from : dp[block]);
+        else
+            s[block] = T::mma32(fk[j / 2], q[j / 2], j == 0 ? f32x16{} : s[block]);
+    };
+    const auto sum = [&](int j) __attribute__((always_inline)) {
+        const int h = j / (2 * NS), e = j % NS;
+        dq[e] = T::mma32(xk[h][e], (j / NS % 2 ? lo : hi)[h], dq[e]);
+    };
+    const auto landed = [] __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const auto step = [&](const char *__restrict__ cur, const char *__restrict__ nxt, char *__restrict__ spare,
+                          int key0) __attribute__((always_inline)) {
+        issue(spare);
+#pragma unroll
+        for (int block = 0; block < 2; ++block) {
+#pragma unroll
+            for (int j = 0; j < 4 * NS; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                score(block ^ 1, j);
+                if (j < 2 * NS)
+                    read_across(cur, block, j);
+#pragma unroll
+                for (int n = 8 + 8 * j / (4 * NS); n < 8 + 8 * (j + 1) / (4 * NS); ++n)
+                    weight(block, n, key0);
             }
-            if (k0 + kTileRows <= wave_free)
-                dq_tile<T, NS, RS, false>(cur, cur + Load::kBytes, along, across, q, d, dq, k0, limit, lse2, delta,
-                                          a.scale2, c);
-            else if (k0 < wave_end)
-                dq_tile<T, NS, RS, true>(cur, cur + Load::kBytes, along, across, q, d, dq, k0, limit, lse2, delta,
-                                         a.scale2, c);
-        };
-        step(lds + turn * (2 * Load::kBytes), lds + (turn ^ 1) * (2 * Load::kBytes));
+#pragma unroll
+            for (int j = 0; j < 4 * NS; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                sum(j);
+                read_along(nxt, block, j);
+                if (j >= 2 * NS) // (the sums with hi[0] and lo[0] are behind)
+#pragma unroll
+                    for (int n = 8 * (j - 2 * NS) / (2 * NS); n < 8 * (j + 1 - 2 * NS) / (2 * NS); ++n)
+                        weight(block ^ 1, n, block ? key0 + kTileRows : key0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (0 < end) {
+        issue(lds);
+        issue(lds + BUF);
+        landed();
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            read_along(lds, 0, j);
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            score(0, j);
+#pragma unroll
+        for (int j = 0; j < 4 * NS; ++j)
+            read_along(lds, 1, j);
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+            weight(0, n, 0);
+        uint32_t at = 0;
+        for (int k0 = 0; k0 < end; k0 += kTileRows) {
+            const uint32_t nxt = at == 2 * BUF ? 0 : at + BUF, spare = nxt == 2 * BUF ? 0 : nxt + BUF;
+            landed(); // the next tile is here, and nobody reads the one before this any more
+            step(lds + at, lds + nxt, lds + spare, k0);
+            at = nxt;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70); // (no load into LDS may outlive the workgroup)
     }
+    rest = halves_sum(rest);
+    if (in && lane < 32)
+        a.minus[ri] = minus - rest / c;
     if (r < rows)
         store_row<T, NS>(a.dq + row_offset(a.sdq, b, head, token), dq, a.dim, a.scale / c);
 }
 
 struct Layout {
-    size_t delta, bound, part, total;
-    int bounds_q, bounds_v, head_splits;
+    size_t minus, lse2, bound, part, total;
+    int q_pad, bounds_q, bounds_v, head_splits;
 };
 size_t align(size_t v) { return (v + 255) / 256 * 256; }
 
 Layout layout(const dnnseq_attention_desc &d)
 {
     Layout l = {};
-    const size_t rows_q = (size_t)d.batch * d.q_heads * d.q_len, rows_v = (size_t)d.batch * d.kv_heads * d.kv_len;
+    const size_t q_tiles = ((size_t)d.q_len + kTileRows - 1) / kTileRows, rows_v = (size_t)d.batch * d.kv_heads * d.kv_len;
     const bool half = d.dtype == DNNSEQ_FP16;
-    l.bounds_q = (int)((rows_q + 15) / 16);
-    l.bounds_v = half ? (int)((rows_v + 15) / 16) : 0;
-    l.bound = align(rows_q * 4);
+    l.q_pad = (int)q_tiles * kTileRows;
+    l.bounds_q = (int)(d.batch * d.q_heads * q_tiles);
+    l.bounds_v = half ? d.batch * d.kv_heads * ((d.kv_len + kTileRows - 1) / kTileRows) : 0;
+    l.lse2 = align((size_t)d.batch * d.q_heads * l.q_pad * 4);
+    l.bound = 2 * l.lse2;
     l.part = l.bound + (half ? align(((size_t)l.bounds_q + l.bounds_v + 2) * 4) : 0);
     // a group's heads over several workgroups until there are two for every CU
     const int group = d.q_heads / d.kv_heads;
@@ -451,17 +608,20 @@ hipError_t backward(const Backward &a, hipStream_t st)
         if (T::kHalf)
             attn_bound_kernel<<<2, 1024, 0, st>>>(a);
     }
+    if (a.q_len) {
+        const int items = a.batch * a.kv_heads * (int)(((int64_t)a.q_len * a.group + 127) / 128);
+        attn_dq_kernel<T, NS><<<items, 256, 0, st>>>(a);
+    }
     if (a.kv_len) {
         const int items = a.batch * a.kv_heads * ((a.kv_len + 127) / 128) * a.head_splits;
-        attn_dkv_kernel<T, NS><<<items, 256, 0, st>>>(a);
+        if (a.causal)
+            attn_dkv_kernel<T, NS, true><<<items, 256, 0, st>>>(a);
+        else
+            attn_dkv_kernel<T, NS, false><<<items, 256, 0, st>>>(a);
         if (a.head_splits > 1) {
             const size_t units = (size_t)a.batch * a.kv_heads * a.kv_len * a.dim / 8;
             attn_dkv_sum_kernel<T><<<dim3((unsigned)((units + 255) / 256), 2), 256, 0, st>>>(a);
         }
-    }
-    if (a.q_len) {
-        const int items = a.batch * a.kv_heads * (int)(((int64_t)a.q_len * a.group + 127) / 128);
-        attn_dq_kernel<T, NS><<<items, 256, 0, st>>>(a);
     }
     return hipGetLastError();
 }
@@ -503,8 +663,8 @@ hipError_t launch_attention_backward(const dnnseq_attention_desc &d, const void 
     a.batch = d.batch, a.q_heads = d.q_heads, a.kv_heads = d.kv_heads, a.group = d.q_heads / d.kv_heads;
     a.q_len = d.q_len, a.kv_len = d.kv_len, a.dim = d.head_dim, a.causal = d.causal;
     a.scale = d.scale, a.scale2 = d.scale * kLog2e;
-    a.delta = (float *)(ws + l.delta), a.bound = (float *)(ws + l.bound);
-    a.bounds_q = l.bounds_q, a.bounds_v = l.bounds_v, a.head_splits = l.head_splits;
+    a.minus = (float *)(ws + l.minus), a.lse2 = (float *)(ws + l.lse2), a.bound = (float *)(ws + l.bound);
+    a.q_pad = l.q_pad, a.bounds_q = l.bounds_q, a.bounds_v = l.bounds_v, a.head_splits = l.head_splits;
     a.part = l.head_splits > 1 ? (float *)(ws + l.part) : nullptr;
     return d.dtype == DNNSEQ_FP16 ? backward_dim<FP16>(a, st) : backward_dim<BF16>(a, st);
 }
