@@ -42,28 +42,41 @@ __device__ __forceinline__ int64_t row_offset(const dnnseq_stride &s, int b, int
     return b * s.batch + head * s.head + token * s.token;
 }
 
-// One tile of 64 keys for 32 rows: `limit` is one past the last key the lane's row sees.
-template <class T, int NS, int RS, bool MASK>
+// One tile of 64 keys for 32 rows: `limit` is one past the last key the lane's row sees.  Operands are read
+// from LDS a phase ahead of their products, and the second block's probabilities are taken while the
+// first block's are multiplied (the barriers keep the order; left to itself the compiler waits for each
+// read in front of its product: 163 us for 2 x 16 heads x 4093 x 128, causal).
+template <class T, int NS, int RS>
 __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const char *__restrict__ vt,
                                              const AlongReader<RS> &along, const AcrossReader<RS> &across,
-                                             const u32x4 (&q)[2 * NS], f32x16 (&acc)[NS], float &m, float &l, int key0,
-                                             int limit, float scale2)
+                                             const u32x4 (&q)[2 * NS], f32x16 (&acc)[NS], float &m, float &l,
+                                             bool masked, int key0, int limit, float scale2)
 {
-    f32x16 s[2];
+    f32x16 s[2] = {};
+    u32x4 k[2 * NS], v[2 * NS];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        s[b] = f32x16{};
+    for (int i = 0; i < 2 * NS; ++i)
+        k[i] = along.get(kt, 0, i);
 #pragma unroll
-        for (int i = 0; i < 2 * NS; ++i)
-            s[b] = T::mma32(along.get(kt, b, i), q[i], s[b]);
+    for (int i = 0; i < 2 * NS; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        s[0] = T::mma32(k[i], q[i], s[0]);
+        k[i] = along.get(kt, 1, i);
     }
-    if (MASK) {
-        const int j0 = key0 + (threadIdx.x % kWave) / 32 * 4;
+#pragma unroll
+    for (int i = 0; i < 2 * NS; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        s[1] = T::mma32(k[i], q[i], s[1]);
+        v[i] = across.get(vt, i / NS, i % NS);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) {
+        const int seen = limit - key0 - (threadIdx.x % kWave) / 32 * 4;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                s[b][r] = j0 + 32 * b + 8 * (r / 4) + r % 4 < limit ? s[b][r] : -INFINITY;
+                s[b][r] = 32 * b + 8 * (r / 4) + r % 4 < seen ? s[b][r] : -INFINITY;
     }
     float top = -INFINITY;
 #pragma unroll
@@ -85,22 +98,31 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
                 acc[e][r] *= f;
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    u32x4 p[2][2]; // rounded to the operands' type: p is at most 2^8, its error 2^-8 or 2^-11 of it
+    const auto weight = [&](int b, int r) __attribute__((always_inline)) {
+        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], scale2, -ref));
+        l += s[b][r];
+        if (r % 2)
+            p[b][half_of(r)][pair_of(r)] = T::pack(s[b][r - 1], s[b][r]);
+    };
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int r = 0; r < 16; ++r)
+        weight(0, r);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], scale2, -ref));
-            l += s[b][r];
-        }
+    for (int j = 0; j < 2 * NS; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        acc[j % NS] = T::mma32(v[j], p[0][j / NS], acc[j % NS]);
+        v[j] = across.get(vt, 2 + j / NS, j % NS);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            // rounded to the operands' type: p is at most 2^8, its error 2^-8 or 2^-11 of it
-            const u32x4 p = pack_half<T>(s[b], h);
-#pragma unroll
-            for (int e = 0; e < NS; ++e)
-                acc[e] = T::mma32(across.get(vt, 2 * b + h, e), p, acc[e]);
-        }
+        for (int r = 16 * j / (2 * NS); r < 16 * (j + 1) / (2 * NS); ++r)
+            weight(1, r);
     }
+#pragma unroll
+    for (int j = 0; j < 2 * NS; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        acc[j % NS] = T::mma32(v[j], p[1][j / NS], acc[j % NS]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <class T, int NS>
@@ -161,10 +183,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Forward a)
                 lk.load(n, k0 + kTileRows, kl);
                 lv.load(n + Load::kBytes, k0 + kTileRows, kl);
             }
-            if (k0 + kTileRows <= wave_free)
-                forward_tile<T, NS, RS, false>(c, c + Load::kBytes, along, across, q, acc, m, l, k0, limit, a.scale2);
-            else if (k0 < wave_end)
-                forward_tile<T, NS, RS, true>(c, c + Load::kBytes, along, across, q, acc, m, l, k0, limit, a.scale2);
+            if (k0 < wave_end)
+                forward_tile<T, NS, RS>(c, c + Load::kBytes, along, across, q, acc, m, l, k0 + kTileRows > wave_free, k0,
+                                        limit, a.scale2);
         };
         step(cur, nxt);
     }

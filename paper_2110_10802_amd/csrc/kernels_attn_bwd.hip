@@ -422,12 +422,12 @@ __global__ __launch_bounds__(256) void attn_dkv_sum_kernel(Backward a)
 // precision of its own rounding, where one rounding of ds costs as much again.  On the way the rows' sums
 // of ds give what delta lacks, o having been rounded: attn_dkv reads the sum.
 template <class T, int NS>
-__global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dq_kernel(Backward a)
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
 {
     constexpr int RS = NS > 2 ? 128 : 64, ROWS = 128;
     typedef TileLoader<RS, 256> Load;
     constexpr int BUF = 2 * Load::kBytes;
-    __shared__ __attribute__((aligned(256))) char lds[3 * BUF]; // [3][keys, values]
+    __shared__ __attribute__((aligned(256))) char lds[2 * BUF]; // [2][keys, values]
     const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
     const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
     const int unit = item / tiles, b = unit / a.kv_heads, g = unit % a.kv_heads;
@@ -461,110 +461,58 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dq_kernel(Backward a
     AcrossReader<RS> across;
     along.init();
     across.init();
-    f32x16 dq[NS], from; // from: -delta, where dp starts
+    f32x16 dq[NS];
 #pragma unroll
     for (int e = 0; e < NS; ++e)
         dq[e] = f32x16{};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        from[i] = minus;
-    int nk = 0; // first key of the tile that is requested next
-    const auto issue = [&](char *__restrict__ buf) __attribute__((always_inline)) {
-        lk.load(buf, 0, kl - nk); // (past the end: zeros, no memory is read)
-        lv.load(buf + Load::kBytes, 0, kl - nk);
-        nk += kTileRows;
-        lk.base += (int64_t)kTileRows * lk.pitch;
-        lv.base += (int64_t)kTileRows * lv.pitch;
-    };
-    f32x16 s[2], dp[2];
-    u32x4 fk[2 * NS], fv[2 * NS], xk[2][NS], hi[2], lo[2];
-    const auto weight = [&](int block, int n, int key0) __attribute__((always_inline)) {
-        const int r = n % 8 / 4 * 8 + n / 8 * 4 + n % 4;
-        float p = __builtin_amdgcn_exp2f(fmaf(s[block][r], scale2, -lse2));
-        p = 32 * block + 8 * (r / 4) + r % 4 < limit - key0 - 4 * half ? p : 0.f;
-        dp[block][r] *= p;
-        if (T::kHalf)
-            dp[block][r] *= c;
-        rest += dp[block][r];
-        if (n % 2) {
-            const float x = dp[block][r - 1], y = dp[block][r];
-            const uint32_t v = T::pack(x, y);
-            hi[half_of(r)][pair_of(r)] = v;
-            lo[half_of(r)][pair_of(r)] = T::pack(x - T::lo(v), y - T::hi(v));
-        }
-    };
-    const auto read_along = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
-        (j % 2 ? fv : fk)[j / 2] = along.get(buf + j % 2 * Load::kBytes, block, j / 2);
-    };
-    const auto read_across = [&](const char *__restrict__ buf, int block, int j) __attribute__((always_inline)) {
-        xk[j / NS][j % NS] = across.get(buf, 2 * block + j / NS, j % NS);
-    };
-    const auto score = [&](int block, int j) __attribute__((always_inline)) {
-        if (j % 2)
-            dp[block] = T::mma32(fv[j / 2], d[j / 2], j == 1 ? from : dp[block]);
-        else
-            s[block] = T::mma32(fk[j / 2], q[j / 2], j == 0 ? f32x16{} : s[block]);
-    };
-    const auto sum = [&](int j) __attribute__((always_inline)) {
-        const int h = j / (2 * NS), e = j % NS;
-        dq[e] = T::mma32(xk[h][e], (j / NS % 2 ? lo : hi)[h], dq[e]);
-    };
-    const auto landed = [] __attribute__((always_inline)) {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070); // vmcnt(0), lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-    const auto step = [&](const char *__restrict__ cur, const char *__restrict__ nxt, char *__restrict__ spare,
-                          int key0) __attribute__((always_inline)) {
-        issue(spare);
+    const auto step = [&](const char *__restrict__ cur, char *__restrict__ nxt, int key0) __attribute__((always_inline)) {
+        lk.load(nxt, key0 + kTileRows, kl); // (past the end: zeros, no memory is read)
+        lv.load(nxt + Load::kBytes, key0 + kTileRows, kl);
 #pragma unroll
         for (int block = 0; block < 2; ++block) {
+            f32x16 s = {}, dp = {};
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int j = 0; j < 4 * NS; ++j) {
-                __builtin_amdgcn_sched_barrier(0);
-                score(block ^ 1, j);
-                if (j < 2 * NS)
-                    read_across(cur, block, j);
+            for (int i = 0; i < 2 * NS; ++i)
+                s = T::mma32(along.get(cur, block, i), q[i], s);
 #pragma unroll
-                for (int n = 8 + 8 * j / (4 * NS); n < 8 + 8 * (j + 1) / (4 * NS); ++n)
-                    weight(block, n, key0);
-            }
+            for (int i = 0; i < 2 * NS; ++i)
+                dp = T::mma32(along.get(cur + Load::kBytes, block, i), d[i], dp);
+            __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-            for (int j = 0; j < 4 * NS; ++j) {
-                __builtin_amdgcn_sched_barrier(0);
-                sum(j);
-                read_along(nxt, block, j);
-                if (j >= 2 * NS) // (the sums with hi[0] and lo[0] are behind)
+            for (int h = 0; h < 2; ++h) {
+                u32x4 hi, lo;
 #pragma unroll
-                    for (int n = 8 * (j - 2 * NS) / (2 * NS); n < 8 * (j + 1 - 2 * NS) / (2 * NS); ++n)
-                        weight(block ^ 1, n, block ? key0 + kTileRows : key0);
+                for (int n = 0; n < 8; ++n) {
+                    const int r = n / 4 * 8 + h * 4 + n % 4;
+                    float p = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -lse2));
+                    p = 32 * block + 8 * (r / 4) + r % 4 < limit - key0 - 4 * half ? p : 0.f;
+                    dp[r] = p * (dp[r] + minus);
+                    if (T::kHalf)
+                        dp[r] *= c;
+                    rest += dp[r];
+                    if (n % 2) {
+                        const uint32_t v = T::pack(dp[r - 1], dp[r]);
+                        hi[n / 2] = v;
+                        lo[n / 2] = T::pack(dp[r - 1] - T::lo(v), dp[r] - T::hi(v));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < NS; ++e) {
+                    const u32x4 x = across.get(cur, 2 * block + h, e);
+                    dq[e] = T::mma32(x, hi, dq[e]);
+                    dq[e] = T::mma32(x, lo, dq[e]);
+                }
             }
         }
-        __builtin_amdgcn_sched_barrier(0);
     };
     if (0 < end) {
-        issue(lds);
-        issue(lds + BUF);
-        landed();
-#pragma unroll
-        for (int j = 0; j < 4 * NS; ++j)
-            read_along(lds, 0, j);
-#pragma unroll
-        for (int j = 0; j < 4 * NS; ++j)
-            score(0, j);
-#pragma unroll
-        for (int j = 0; j < 4 * NS; ++j)
-            read_along(lds, 1, j);
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-            weight(0, n, 0);
-        uint32_t at = 0;
-        for (int k0 = 0; k0 < end; k0 += kTileRows) {
-            const uint32_t nxt = at == 2 * BUF ? 0 : at + BUF, spare = nxt == 2 * BUF ? 0 : nxt + BUF;
-            landed(); // the next tile is here, and nobody reads the one before this any more
-            step(lds + at, lds + nxt, lds + spare, k0);
-            at = nxt;
+        lk.load(lds, 0, kl);
+        lv.load(lds + Load::kBytes, 0, kl);
+        for (int k0 = 0, turn = 0; k0 < end; k0 += kTileRows, turn ^= 1) {
+            __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
+            __syncthreads();                    // and everyone's; the other buffer is no longer read
+            step(lds + turn * BUF, lds + (turn ^ 1) * BUF, k0);
         }
         __builtin_amdgcn_s_waitcnt(0x0f70); // (no load into LDS may outlive the workgroup)
     }
