@@ -140,12 +140,32 @@ __device__ __forceinline__ int clamp_len(const int32_t *lens, int b, int top)
     return lens ? min(max(lens[b], 0), top) : top;
 }
 
-// Workgroup -> work item: each of the eight XCDs (workgroup b runs on XCD b % 8) gets a run of
-// consecutive items, so the items that read the same keys share an L2.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n)
+// Workgroups in groups that read the same keys (or the same rows), `size` to a group.  Workgroup b runs on
+// XCD b % 8.  `spread`: whole groups go to the XCDs in turn, so a group shares an L2 and requests of
+// different lengths load all XCDs alike (8 requests of 205 to 512 tokens: 76 us for a training step,
+// against 79 with each request on one XCD).  With few groups, that would leave XCDs without work: then
+// each XCD takes a run of consecutive workgroups.
+struct Groups {
+    int groups, size, spread;
+};
+inline Groups make_groups(int64_t groups, int64_t size)
 {
-    const uint32_t x = b % 8, each = n / 8, more = n % 8;
-    return x * each + min(x, more) + b / 8;
+    return {(int)groups, (int)size, groups % 8 == 0 || groups >= 32};
+}
+inline unsigned grid_of(const Groups &o) { return (unsigned)((o.spread ? (o.groups + 7) / 8 * 8 : o.groups) * o.size); }
+// false: a workgroup past the last group
+__device__ __forceinline__ bool item_of(const Groups &o, int &group, int &item)
+{
+    const uint32_t b = blockIdx.x, x = b % 8;
+    if (o.spread) {
+        group = x + b / 8 / o.size * 8;
+        item = b / 8 % o.size;
+        return group < o.groups;
+    }
+    const uint32_t n = o.groups * o.size, each = n / 8, more = n % 8, t = x * each + min(x, more) + b / 8;
+    group = t / o.size;
+    item = t % o.size;
+    return true;
 }
 
 } // namespace dsq

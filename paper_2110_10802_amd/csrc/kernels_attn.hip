@@ -28,6 +28,7 @@ struct Forward {
     dnnseq_stride sq, sk, sv, so;
     int batch, q_heads, kv_heads, group, q_len, kv_len, dim, causal;
     float scale2; // scale * log2 e
+    Groups order; // attn_fwd: (request, key head, split), its tiles of rows
     int splits, per_split;   // keys per split, a multiple of 64
     float *part_o, *part_lse; // [splits][batch][q_heads][q_len][dim], [splits][batch][q_heads][q_len]
 };
@@ -57,18 +58,25 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i)
         k[i] = along.get(kt, 0, i);
+    __builtin_amdgcn_s_setprio(1); // the other wavefront of the SIMD has its vector phase meanwhile (160 -> 147 us)
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         s[0] = T::mma32(k[i], q[i], s[0]);
         k[i] = along.get(kt, 1, i);
     }
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         s[1] = T::mma32(k[i], q[i], s[1]);
         v[i] = across.get(vt, i / NS, i % NS);
+        if (i) // (the first block's last product is done)
+#pragma unroll
+            for (int r = 16 * (i - 1) / (2 * NS - 1); r < 16 * i / (2 * NS - 1); ++r)
+                top = fmaxf(top, s[0][r]);
     }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     if (masked) {
         const int seen = limit - key0 - (threadIdx.x % kWave) / 32 * 4;
@@ -77,13 +85,14 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[b][r] = 32 * b + 8 * (r / 4) + r % 4 < seen ? s[b][r] : -INFINITY;
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
+        top = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-            top = fmaxf(top, s[b][r]);
+            top = fmaxf(top, s[0][r]);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        top = fmaxf(top, s[1][r]);
     top = halves_max(top) * scale2;
     // The reference point m follows the maximum only when that outgrows it by 2^8: p and the sums stay
     // far inside fp32 and fp16, and most tiles leave the accumulators alone.
@@ -108,6 +117,7 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
 #pragma unroll
     for (int r = 0; r < 16; ++r)
         weight(0, r);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < 2 * NS; ++j) {
         __builtin_amdgcn_sched_barrier(0);
@@ -122,6 +132,7 @@ __device__ __forceinline__ void forward_tile(const char *__restrict__ kt, const 
         __builtin_amdgcn_sched_barrier(0);
         acc[j % NS] = T::mma32(v[j], p[1][j / NS], acc[j % NS]);
     }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -131,13 +142,15 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Forward a)
     constexpr int RS = NS > 2 ? 128 : 64, ROWS = 128;
     typedef TileLoader<RS, 256> Load;
     __shared__ __attribute__((aligned(256))) char lds[4 * Load::kBytes]; // [2][keys, values]
-    const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
-    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
-    const int unit = item / tiles, b = unit / a.kv_heads, g = unit % a.kv_heads;
-    const int r0 = (tiles - 1 - item % tiles) * ROWS; // the rows that see most keys first
+    const int rows = a.q_len * a.group;
+    int group, tile;
+    if (!item_of(a.order, group, tile))
+        return;
+    const int unit = group / a.splits, split = (group + unit) % a.splits, b = unit / a.kv_heads, g = unit % a.kv_heads;
+    const int r0 = (a.order.size - 1 - tile) * ROWS; // the rows that see most keys first
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
     const int lane = threadIdx.x % kWave, w = wave_id();
-    const int first = blockIdx.y * a.per_split, last = min(kl, first + a.per_split);
+    const int first = split * a.per_split, last = min(kl, first + a.per_split);
     // one past the last key that a row sees
     const auto limit_of = [&](int r) {
         const int t = r / a.group;
@@ -196,7 +209,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Forward a)
     const float lse = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
     const size_t ri = row_index(a, b, g, r);
     if (a.part_o) {
-        const size_t all = (size_t)a.batch * a.q_heads * a.q_len, at = blockIdx.y * all + ri;
+        const size_t all = (size_t)a.batch * a.q_heads * a.q_len, at = split * all + ri;
         if (lane < 32)
             a.part_lse[at] = lse;
         if (lse == -INFINITY)
@@ -245,8 +258,10 @@ __global__ __launch_bounds__(256) void attn_token_kernel(Forward a)
     constexpr int VBYTES = kChunk * RS * 2;
     __shared__ __attribute__((aligned(256))) char lds[4 * 2 * VBYTES]; // [4 wavefronts][2][32 values]
     __shared__ float wm[4][16], wl[4][16];
-    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
-    const int split = item % a.splits, unit = item / a.splits, b = unit / a.kv_heads, g = unit % a.kv_heads;
+    // Nothing is shared between workgroups.  The parts of a request go to the XCDs in turn (workgroup b runs
+    // on XCD b % 8), and those of the next one are turned by one: requests of different lengths, whose last
+    // parts are empty, leave no XCD idle.
+    const int unit = blockIdx.x / a.splits, split = (blockIdx.x + unit) % a.splits, b = unit / a.kv_heads, g = unit % a.kv_heads;
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
     const int rows = a.q_len * a.group, lane = threadIdx.x % kWave, w = wave_id();
     const int first = split * a.per_split, last = min(kl, first + a.per_split);
@@ -423,7 +438,8 @@ __global__ __launch_bounds__(256) void attn_token_kernel(Forward a)
             u32x4{T::pack(v[0], v[1]), T::pack(v[2], v[3]), T::pack(v[4], v[5]), T::pack(v[6], v[7])};
 }
 
-// The parts of a row joined: weights exp(lse_s - lse).  A wavefront per row, two elements per lane.
+// The parts of a row joined: weights exp(lse_s - lse).  A wavefront per row; a lane holds the weight of
+// a part (and of the 64th after it) and two elements.
 template <class T>
 __global__ __launch_bounds__(256) void attn_combine_kernel(Forward a)
 {
@@ -433,22 +449,37 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(Forward a)
         return;
     const int lane = threadIdx.x % kWave, c = lane * 2;
     float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s)
+    for (int s = lane; s < a.splits; s += kWave)
         top = fmaxf(top, a.part_lse[s * all + ri]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1)
+        top = fmaxf(top, __shfl_xor(top, o, kWave));
     float total = 0.f, x = 0.f, y = 0.f;
     if (top != -INFINITY)
-        for (int s = 0; s < a.splits; ++s) {
-            const float e = a.part_lse[s * all + ri];
-            if (e == -INFINITY)
-                continue;
+        for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+            const float e = s0 + lane < a.splits ? a.part_lse[(s0 + lane) * all + ri] : -INFINITY;
             const float f = __builtin_amdgcn_exp2f((e - top) * kLog2e);
             total += f;
-            if (c < a.dim) {
-                const f32x2 v = *(const f32x2 *)(a.part_o + (s * all + ri) * a.dim + c);
-                x = fmaf(f, v[0], x);
-                y = fmaf(f, v[1], y);
+            const int n = min(a.splits - s0, kWave);
+            for (int s = 0; s < n; s += 8) {
+                float w[8];
+                f32x2 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    w[j] = s + j < n ? __shfl(f, s + j, kWave) : 0.f;
+                    // (a part that saw nothing has written nothing)
+                    v[j] = c < a.dim && w[j] != 0.f
+                               ? *(const f32x2 *)(a.part_o + ((s0 + s + j) * all + ri) * a.dim + c)
+                               : f32x2{0.f, 0.f};
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x = fmaf(w[j], v[j][0], x);
+                    y = fmaf(w[j], v[j][1], y);
+                }
             }
         }
+    total = mbk::wave_sum(total);
     const float inv = total == 0.f ? 0.f : 1.0f / total;
     const int token = ri % a.q_len, head = ri / a.q_len % a.q_heads, b = ri / a.q_len / a.q_heads;
     if (a.lse && lane == 0)
@@ -459,7 +490,8 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(Forward a)
 
 struct Plan {
     bool token;
-    int items, splits, per_split;
+    int splits, per_split;
+    Groups order;
 };
 Plan plan(const dnnseq_attention_desc &d)
 {
@@ -467,16 +499,16 @@ Plan plan(const dnnseq_attention_desc &d)
     const int64_t rows = (int64_t)d.q_len * (d.q_heads / d.kv_heads);
     p.token = rows <= 16;
     const int64_t items = (int64_t)d.batch * d.kv_heads * (p.token ? 1 : (rows + 127) / 128);
-    p.items = (int)items;
     // keys per workgroup: enough workgroups to fill the 256 CUs, but no shorter than what hides a
     // workgroup's start and the joining
-    const int64_t want = std::max<int64_t>(1, (p.token ? 2048 : 512) / std::max<int64_t>(items, 1));
+    const int64_t want = std::max<int64_t>(1, (p.token ? 4096 : 512) / std::max<int64_t>(items, 1));
     const int64_t least = 512;
     const int64_t per = std::max(least, ((d.kv_len + want - 1) / want + 63) / 64 * 64);
     p.per_split = (int)per;
     p.splits = (int)std::max<int64_t>(1, (d.kv_len + per - 1) / per);
     if (p.splits == 1)
         p.per_split = (std::max(d.kv_len, 1) + 63) / 64 * 64;
+    p.order = make_groups((int64_t)d.batch * d.kv_heads * p.splits, p.token ? 1 : (rows + 127) / 128);
     return p;
 }
 
@@ -484,9 +516,9 @@ template <class T, int NS>
 hipError_t forward(Forward a, const Plan &p, hipStream_t st)
 {
     if (p.token)
-        attn_token_kernel<T, NS><<<p.items * p.splits, 256, 0, st>>>(a);
+        attn_token_kernel<T, NS><<<p.order.groups, 256, 0, st>>>(a);
     else
-        attn_fwd_kernel<T, NS><<<dim3(p.items, p.splits), 256, 0, st>>>(a);
+        attn_fwd_kernel<T, NS><<<grid_of(p.order), 256, 0, st>>>(a);
     if (p.splits > 1) {
         const size_t rows = (size_t)a.batch * a.q_heads * a.q_len;
         attn_combine_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a);
@@ -531,7 +563,7 @@ hipError_t launch_attention_forward(const dnnseq_attention_desc &d, const void *
     a.batch = d.batch, a.q_heads = d.q_heads, a.kv_heads = d.kv_heads, a.group = d.q_heads / d.kv_heads;
     a.q_len = d.q_len, a.kv_len = d.kv_len, a.dim = d.head_dim, a.causal = d.causal;
     a.scale2 = d.scale * kLog2e;
-    a.splits = p.splits, a.per_split = p.per_split;
+    a.splits = p.splits, a.per_split = p.per_split, a.order = p.order;
     if (p.splits > 1) {
         a.part_o = (float *)scratch;
         a.part_lse = a.part_o + (size_t)p.splits * d.batch * d.q_heads * d.q_len * d.head_dim;

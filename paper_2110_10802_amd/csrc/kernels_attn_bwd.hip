@@ -34,6 +34,9 @@ struct Backward {
     int q_pad;           // q_len to a whole number of tiles
     float *bound;    // fp16: [bounds] squares of row norms, their maxima per workgroup (dout, then v)
     int bounds_q, bounds_v;
+    // groups are (request, key head): attn_dq's items the tiles of their rows, attn_dkv's the tiles of their
+    // keys times the parts of the heads
+    Groups q_order, kv_order;
     int head_splits; // workgroups that share the heads of a group in attn_dkv
     float *part;     // [head_splits][dk, dv][batch][kv_heads][kv_len][dim]
 };
@@ -184,10 +187,11 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward 
     typedef TileLoader<RS, 256> Load;
     constexpr int LSE = 2 * Load::kBytes, DELTA = LSE + kTileRows * 4, BUF = DELTA + kTileRows * 4;
     __shared__ __attribute__((aligned(256))) char lds[3 * BUF]; // [3][q, dout, lse2, delta]
-    const int tiles = (a.kv_len + KEYS - 1) / KEYS;
-    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
-    const int hs = item % a.head_splits, tile = item / a.head_splits % tiles, unit = item / a.head_splits / tiles;
-    const int b = unit / a.kv_heads, g = unit % a.kv_heads;
+    // (an item is a part of the heads of one tile: the heaviest tiles of all heads come first)
+    int unit, item;
+    if (!item_of(a.kv_order, unit, item))
+        return;
+    const int hs = item % a.head_splits, tile = item / a.head_splits, b = unit / a.kv_heads, g = unit % a.kv_heads;
     const int key0 = tile * KEYS; // (the first keys are seen by most rows: they come first)
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
     const int lane = threadIdx.x % kWave, w = wave_id(), half = lane / 32;
@@ -428,10 +432,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
     typedef TileLoader<RS, 256> Load;
     constexpr int BUF = 2 * Load::kBytes;
     __shared__ __attribute__((aligned(256))) char lds[2 * BUF]; // [2][keys, values]
-    const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
-    const uint32_t item = xcd_order(blockIdx.x, gridDim.x);
-    const int unit = item / tiles, b = unit / a.kv_heads, g = unit % a.kv_heads;
-    const int r0 = (tiles - 1 - item % tiles) * ROWS; // the rows that see most keys first
+    const int rows = a.q_len * a.group;
+    int unit, tile;
+    if (!item_of(a.q_order, unit, tile))
+        return;
+    const int b = unit / a.kv_heads, g = unit % a.kv_heads;
+    const int r0 = (a.q_order.size - 1 - tile) * ROWS; // the rows that see most keys first
     const int ql = clamp_len(a.q_lens, b, a.q_len), kl = clamp_len(a.kv_lens, b, a.kv_len);
     const int lane = threadIdx.x % kWave, w = wave_id(), half = lane / 32;
     const auto limit_of = [&](int r) { // one past the last key that a row sees
@@ -556,16 +562,13 @@ hipError_t backward(const Backward &a, hipStream_t st)
         if (T::kHalf)
             attn_bound_kernel<<<2, 1024, 0, st>>>(a);
     }
-    if (a.q_len) {
-        const int items = a.batch * a.kv_heads * (int)(((int64_t)a.q_len * a.group + 127) / 128);
-        attn_dq_kernel<T, NS><<<items, 256, 0, st>>>(a);
-    }
+    if (a.q_len)
+        attn_dq_kernel<T, NS><<<grid_of(a.q_order), 256, 0, st>>>(a);
     if (a.kv_len) {
-        const int items = a.batch * a.kv_heads * ((a.kv_len + 127) / 128) * a.head_splits;
         if (a.causal)
-            attn_dkv_kernel<T, NS, true><<<items, 256, 0, st>>>(a);
+            attn_dkv_kernel<T, NS, true><<<grid_of(a.kv_order), 256, 0, st>>>(a);
         else
-            attn_dkv_kernel<T, NS, false><<<items, 256, 0, st>>>(a);
+            attn_dkv_kernel<T, NS, false><<<grid_of(a.kv_order), 256, 0, st>>>(a);
         if (a.head_splits > 1) {
             const size_t units = (size_t)a.batch * a.kv_heads * a.kv_len * a.dim / 8;
             attn_dkv_sum_kernel<T><<<dim3((unsigned)((units + 255) / 256), 2), 256, 0, st>>>(a);
@@ -611,6 +614,9 @@ hipError_t launch_attention_backward(const dnnseq_attention_desc &d, const void 
     a.batch = d.batch, a.q_heads = d.q_heads, a.kv_heads = d.kv_heads, a.group = d.q_heads / d.kv_heads;
     a.q_len = d.q_len, a.kv_len = d.kv_len, a.dim = d.head_dim, a.causal = d.causal;
     a.scale = d.scale, a.scale2 = d.scale * kLog2e;
+    const int64_t units = (int64_t)d.batch * d.kv_heads;
+    a.q_order = make_groups(units, ((int64_t)d.q_len * a.group + 127) / 128);
+    a.kv_order = make_groups(units, (int64_t)((d.kv_len + 127) / 128) * l.head_splits);
     a.minus = (float *)(ws + l.minus), a.lse2 = (float *)(ws + l.lse2), a.bound = (float *)(ws + l.bound);
     a.q_pad = l.q_pad, a.bounds_q = l.bounds_q, a.bounds_v = l.bounds_v, a.head_splits = l.head_splits;
     a.part = l.head_splits > 1 ? (float *)(ws + l.part) : nullptr;

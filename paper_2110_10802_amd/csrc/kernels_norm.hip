@@ -279,22 +279,28 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
     }
 }
 
-// out[c] = sum over parts of in[parts][cols]; y: gamma or beta.  A workgroup per 64 columns, every
-// wavefront takes each fourth part.
-__global__ __launch_bounds__(256) void norm_sum_kernel(const float *pgamma, const float *pbeta, int parts, int cols,
-                                                       float *dgamma, float *dbeta)
+// out[c] = sum over parts of in[parts][cols]; y: gamma or beta.  A workgroup per 64 columns, each of its
+// sixteen wavefronts takes every sixteenth part.
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float *pgamma, const float *pbeta, int parts, int cols,
+                                                        float *dgamma, float *dbeta)
 {
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
     const float *in = blockIdx.y ? pbeta : pgamma;
-    __shared__ float red[4][kWave];
+    __shared__ float red[16][kWave];
     float s = 0.f;
-    if (c < cols)
-        for (int p = w; p < parts; p += 4)
+    if (c < cols) {
+#pragma unroll 8
+        for (int p = w; p < parts; p += 16)
             s += in[(size_t)p * cols + c];
+    }
     red[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < cols)
-        (blockIdx.y ? dbeta : dgamma)[c] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    if (w == 0 && c < cols) {
+#pragma unroll
+        for (int v = 1; v < 16; ++v)
+            s += red[v][lane];
+        (blockIdx.y ? dbeta : dgamma)[c] = s;
+    }
 }
 
 // Threads per row and units per thread for a row length.
@@ -371,7 +377,7 @@ hipError_t launch_norm_backward(const dnnseq_layernorm_desc &d, const void *x, c
                                           : (dx_add ? backward<BF16, true> : backward<BF16, false>);
     if (d.rows)
         f(d, x, dy, gamma, mean, rstd, dx_add, dx, pgamma, pbeta, grid, st);
-    norm_sum_kernel<<<dim3((d.cols + kWave - 1) / kWave, 2), 256, 0, st>>>(pgamma, pbeta, grid, d.cols, dgamma, dbeta);
+    norm_sum_kernel<<<dim3((d.cols + kWave - 1) / kWave, 2), 1024, 0, st>>>(pgamma, pbeta, grid, d.cols, dgamma, dbeta);
     return hipGetLastError();
 }
 
