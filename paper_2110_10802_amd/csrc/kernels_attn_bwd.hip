@@ -546,10 +546,11 @@ Layout layout(const dnnseq_attention_desc &d)
     l.lse2 = align((size_t)d.batch * d.q_heads * l.q_pad * 4);
     l.bound = 2 * l.lse2;
     l.part = l.bound + (half ? align(((size_t)l.bounds_q + l.bounds_v + 2) * 4) : 0);
-    // a group's heads over several workgroups until there are two for every CU
+    // a group's heads over several workgroups until there are two for every CU (more cost more in parts: 2 x 16
+    // heads on 4 key heads x 4093 x 128, four parts 319 + 23 us, two 319 + 14)
     const int group = d.q_heads / d.kv_heads;
     const int64_t items = (int64_t)d.batch * d.kv_heads * ((d.kv_len + 127) / 128);
-    l.head_splits = (int)std::max<int64_t>(1, std::min<int64_t>(group, 1024 / std::max<int64_t>(items, 1)));
+    l.head_splits = (int)std::max<int64_t>(1, std::min<int64_t>(group, 512 / std::max<int64_t>(items, 1)));
     l.total = l.part + (l.head_splits > 1 ? (size_t)l.head_splits * 2 * rows_v * d.head_dim * 4 : 0);
     return l;
 }
