@@ -1,0 +1,208 @@
+"""A transformer layer built from the sequence operators (``dnnseq``): training step and decoding.
+
+    x1 = x + Wo attention(LN1 x) + bo,   y = x1 + W2 act(W1 LN2 x1 + b1) + b2
+
+Parameters, activations and the key/value cache are PyTorch-ROCm tensors (device memory and the
+stream only); every computation runs inside the library: layer normalisation (its backward pass
+adds the gradient of the residual path), linear layers (bias, activation and residual in the
+epilogue, the residual path's gradient in the data gradient's), attention over shared key heads
+with a length for every sequence.
+
+``python -m paper_2110_10802_amd.transformer`` times a training step and a decoding step.
+"""
+from __future__ import annotations
+
+from typing import Dict, Optional
+
+import torch
+
+from . import dnnseq as S
+
+LINEARS = ("q", "k", "v", "o", "1", "2")
+
+
+class TransformerLayer:
+    """Weights, gradients and the buffers of one batch shape.  ``causal``: a decoder layer."""
+
+    def __init__(self, width: int, heads: int, kv_heads: int, hidden: int, activation: str = "gelu",
+                 causal: bool = False, dtype: torch.dtype = torch.bfloat16, eps: float = 1e-5, device: str = "cuda:0",
+                 seed: int = 0):
+        self.width, self.heads, self.kv_heads, self.hidden = width, heads, kv_heads, hidden
+        self.dim = width // heads
+        self.activation, self.causal, self.dtype, self.eps = activation, causal, dtype, eps
+        self.device = torch.device(device)
+        gen = torch.Generator().manual_seed(seed)
+        kv = kv_heads * self.dim
+        sizes = {"q": (width, width), "k": (kv, width), "v": (kv, width), "o": (width, width), "1": (hidden, width),
+                 "2": (width, hidden)}
+        self.params: Dict[str, torch.Tensor] = {}
+        for n, (rows, cols) in sizes.items():
+            self.params["w" + n] = (torch.randn(rows, cols, generator=gen) * cols ** -0.5).to(self.device, dtype)
+            self.params["b" + n] = (0.1 * torch.randn(rows, generator=gen)).to(self.device)
+        for n in ("1", "2"):
+            self.params["gamma" + n] = (1 + 0.1 * torch.randn(width, generator=gen)).to(self.device)
+            self.params["beta" + n] = (0.1 * torch.randn(width, generator=gen)).to(self.device)
+        self.grads = {n: torch.zeros_like(p) for n, p in self.params.items()}
+        self._plans: Dict[tuple, dict] = {}
+
+    # ---- buffers and descriptors of a shape ----------------------------------------------------
+
+    def _empty(self, *shape, dtype=None):
+        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+
+    def _heads(self, t: torch.Tensor, batch: int, heads: int) -> torch.Tensor:
+        """[tokens, heads*dim] as [batch, heads, length, dim] (a view)."""
+        return t.view(batch, -1, heads, self.dim).transpose(1, 2)
+
+    def _plan(self, batch: int, length: int, cache: Optional[torch.Tensor] = None) -> dict:
+        key = (batch, length, None if cache is None else cache.shape)
+        if key in self._plans:
+            return self._plans[key]
+        n, width, kv = batch * length, self.width, self.kv_heads * self.dim
+        p = {"h1": self._empty(n, width), "q": self._empty(n, width), "k": self._empty(n, kv), "v": self._empty(n, kv),
+             "o": self._empty(n, width), "x1": self._empty(n, width), "h2": self._empty(n, width),
+             "z": self._empty(n, self.hidden), "u": self._empty(n, self.hidden), "y": self._empty(n, width),
+             "lse": self._empty(batch, self.heads, length, dtype=torch.float32)}
+        for i in ("1", "2"):
+            p["mean" + i], p["rstd" + i] = self._empty(n, dtype=torch.float32), self._empty(n, dtype=torch.float32)
+        p["norm"] = S.layernorm_desc(p["h1"], self.eps)
+        inputs = {"q": "h1", "k": "h1", "v": "h1", "o": "o", "1": "h2", "2": "u"}
+        p["linear"] = {i: S.linear_desc(p[inputs[i]], self.params["w" + i], self.activation if i == "1" else "none")
+                       for i in LINEARS}
+        need = [S.linear_forward_scratch_bytes(d) for d in p["linear"].values()]
+        p["qh"], p["oh"] = self._heads(p["q"], batch, self.heads), self._heads(p["o"], batch, self.heads)
+        if cache is None:
+            p["kh"], p["vh"] = self._heads(p["k"], batch, self.kv_heads), self._heads(p["v"], batch, self.kv_heads)
+            p.update({"d" + t: torch.empty_like(p[t]) for t in ("h1", "q", "k", "v", "o", "x1", "h2", "u", "y")})
+            p["attention"] = S.attention_desc(p["qh"], p["kh"], p["vh"], p["oh"], causal=self.causal)
+            need += [S.linear_backward_scratch_bytes(d) for d in p["linear"].values()]
+            need += [S.attention_backward_scratch_bytes(p["attention"]), S.layernorm_backward_scratch_bytes(p["norm"])]
+        else:
+            p["attention"] = S.attention_desc(p["qh"], cache[0], cache[1], p["oh"], causal=True)
+        need.append(S.attention_forward_scratch_bytes(p["attention"]))
+        p["scratch"] = self._empty(max(need + [16]), dtype=torch.uint8)
+        self._plans[key] = p
+        return p
+
+    def _linear(self, p, i, x, y, stream, residual=None, z=None):
+        S.linear_forward(p["linear"][i], x, self.params["w" + i], y, bias=self.params["b" + i], residual=residual, z=z,
+                         scratch=p["scratch"], stream=stream)
+
+    def _norm(self, p, i, x, y, stream):
+        S.layernorm_forward(p["norm"], x, self.params["gamma" + i], self.params["beta" + i], y, p["mean" + i],
+                            p["rstd" + i], stream=stream)
+
+    def _feed_forward(self, p, x, stream, keep):
+        """From attention's output on: the projection onto the residual path and the second half."""
+        self._linear(p, "o", p["o"], p["x1"], stream, residual=x)
+        self._norm(p, "2", p["x1"], p["h2"], stream)
+        self._linear(p, "1", p["h2"], p["u"], stream, z=p["z"] if keep else None)
+        self._linear(p, "2", p["u"], p["y"], stream, residual=p["x1"])
+
+    # ---- training --------------------------------------------------------------------------------
+
+    def forward(self, x: torch.Tensor, lens: Optional[torch.Tensor] = None, stream: int = 0) -> torch.Tensor:
+        """x [batch, length, width]; ``lens``: int32 [batch], the sequences' lengths (padding on the
+        right takes no part in attention).  The result is a buffer that the next call of the same
+        shape overwrites."""
+        batch, length, _ = x.shape
+        p = self._plan(batch, length)
+        p["x"], p["lens"] = x.reshape(-1, self.width), lens
+        self._norm(p, "1", p["x"], p["h1"], stream)
+        for i in ("q", "k", "v"):
+            self._linear(p, i, p["h1"], p[i], stream)
+        S.attention_forward(p["attention"], p["q"], p["k"], p["v"], p["o"], lse=p["lse"], q_lens=lens, kv_lens=lens,
+                            scratch=p["scratch"], stream=stream)
+        self._feed_forward(p, p["x"], stream, True)
+        return p["y"].view(x.shape)
+
+    def backward(self, dy: torch.Tensor, stream: int = 0) -> torch.Tensor:
+        """Gradients of sum(y * dy) for the latest ``forward`` of this shape: the parameters' in
+        ``grads``, the input's returned."""
+        batch, length, _ = dy.shape
+        p, w, g = self._plan(batch, length), self.params, self.grads
+        dy2, ws = dy.reshape(-1, self.width), p["scratch"]
+
+        def linear(i, x, d, dx, z=None, add=None):
+            S.linear_backward(p["linear"][i], x, w["w" + i], d, z=z, dx=dx, dx_add=add, dw=g["w" + i], db=g["b" + i],
+                              scratch=ws, stream=stream)
+
+        def norm(i, x, d, dx, add):
+            S.layernorm_backward(p["norm"], x, d, w["gamma" + i], p["mean" + i], p["rstd" + i], dx, g["gamma" + i],
+                                 g["beta" + i], ws, dx_add=add, stream=stream)
+
+        linear("2", p["u"], dy2, p["du"])
+        linear("1", p["h2"], p["du"], p["dh2"], z=p["z"])
+        norm("2", p["x1"], p["dh2"], p["dx1"], dy2)
+        linear("o", p["o"], p["dx1"], p["do"])
+        S.attention_backward(p["attention"], p["q"], p["k"], p["v"], p["o"], p["do"], p["lse"], p["dq"], p["dk"],
+                             p["dv"], ws, q_lens=p["lens"], kv_lens=p["lens"], stream=stream)
+        linear("q", p["h1"], p["dq"], p["dh1"])
+        linear("k", p["h1"], p["dk"], p["dh1"], add=p["dh1"])
+        linear("v", p["h1"], p["dv"], p["dh1"], add=p["dh1"])
+        norm("1", p["x"], p["dh1"], p["dy"], p["dx1"])
+        return p["dy"].view(dy.shape)
+
+    # ---- decoding --------------------------------------------------------------------------------
+
+    def new_cache(self, batch: int, length: int) -> torch.Tensor:
+        """Keys and values [2, batch, kv_heads, length, dim]."""
+        return torch.zeros(2, batch, self.kv_heads, length, self.dim, dtype=self.dtype, device=self.device)
+
+    def decode(self, x: torch.Tensor, cache: torch.Tensor, slots: torch.Tensor, lens: torch.Tensor,
+               stream: int = 0) -> torch.Tensor:
+        """The next tokens [batch, n, width] of every request (n = 1 when generating).  ``slots``
+        [batch, n] (int64): where in the cache their keys and values go; ``lens`` [batch] (int32):
+        the cache's lengths with them.  Runs on torch's current stream, which ``stream`` names."""
+        batch, n, _ = x.shape
+        p = self._plan(batch, n, cache)
+        x2 = x.reshape(-1, self.width)
+        self._norm(p, "1", x2, p["h1"], stream)
+        for i in ("q", "k", "v"):
+            self._linear(p, i, p["h1"], p[i], stream)
+        b = torch.arange(batch, device=self.device)[:, None]
+        for i, t in ((0, p["k"]), (1, p["v"])):
+            cache[i][b, :, slots] = t.view(batch, n, self.kv_heads, self.dim)
+        S.attention_forward(p["attention"], p["q"], cache[0], cache[1], p["o"], kv_lens=lens, scratch=p["scratch"],
+                            stream=stream)
+        self._feed_forward(p, x2, stream, False)
+        return p["y"].view(x.shape)
+
+
+def main() -> None:
+    import time
+
+    def clock(f, n=20):
+        for _ in range(3):
+            f()
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        for _ in range(n):
+            f()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t) / n * 1e6
+
+    stream = torch.cuda.current_stream().cuda_stream
+    layer = TransformerLayer(1024, 16, 16, 4096)
+    x = torch.randn(8, 512, 1024, device="cuda:0").to(layer.dtype)
+    dy = torch.randn_like(x)
+
+    def train():
+        layer.forward(x, stream=stream)
+        layer.backward(dy, stream=stream)
+
+    flops = 3 * 8 * 512 * (2 * 4 * 1024 ** 2 + 2 * 2 * 1024 * 4096 + 4 * 512 * 1024)
+    us = clock(train)
+    print(f"training step, batch 8, sequence 512, width 1024, hidden 4096, bf16: {us:.0f} us, "
+          f"{flops / us / 1e6:.0f} TFLOP/s")
+    decoder = TransformerLayer(1024, 16, 4, 4096, causal=True)
+    cache = decoder.new_cache(16, 4096)
+    token = torch.randn(16, 1, 1024, device="cuda:0").to(decoder.dtype)
+    lens = torch.full((16,), 4096, dtype=torch.int32, device="cuda:0")
+    slots = (lens.long() - 1)[:, None]
+    us = clock(lambda: decoder.decode(token, cache, slots, lens, stream=stream))
+    print(f"decoding step, batch 16, 4 key heads, cache of 4096: {us:.0f} us")
+
+
+if __name__ == "__main__":
+    main()

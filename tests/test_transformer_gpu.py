@@ -1,0 +1,138 @@
+"""The transformer layer that is built from the sequence operators, against the same layer in 64
+bits (torch autograd on the CPU): training with ragged batches, decoding against the training
+forward, other streams, and graph capture."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _layer(**kw):
+    from paper_2110_10802_amd.transformer import TransformerLayer
+    return TransformerLayer(**dict(dict(width=128, heads=8, kv_heads=2, hidden=264), **kw))
+
+
+def _reference(layer, x, lens, dy):
+    p = {n: t.double().cpu().requires_grad_() for n, t in layer.params.items()}
+    x = x.double().cpu().requires_grad_()
+    F = torch.nn.functional
+    B, L, E = x.shape
+    H, G, D = layer.heads, layer.kv_heads, layer.dim
+
+    def lin(i, t):
+        return t @ p["w" + i].T + p["b" + i]
+
+    h = F.layer_norm(x, (E,), p["gamma1"], p["beta1"], layer.eps)
+    q = lin("q", h).view(B, L, H, D).transpose(1, 2)
+    k, v = (lin(i, h).view(B, L, G, D).transpose(1, 2).repeat_interleave(H // G, 1) for i in "kv")
+    i, j = torch.arange(L)[:, None], torch.arange(L)[None]
+    n = torch.tensor(lens)[:, None, None]
+    seen = (i < n) & (j < n)
+    if layer.causal:
+        seen = seen & (j <= i)
+    s = (q @ k.transpose(2, 3) * D ** -0.5).masked_fill(~seen[:, None], -1e30)
+    o = (torch.softmax(s, -1) * seen[:, None]) @ v
+    x1 = x + lin("o", o.transpose(1, 2).reshape(B, L, E))
+    act = {"gelu": F.gelu, "silu": F.silu}[layer.activation]
+    y = x1 + lin("2", act(lin("1", F.layer_norm(x1, (E,), p["gamma2"], p["beta2"], layer.eps))))
+    (y * dy.double().cpu()).sum().backward()
+    return y.detach(), x.grad, {n: t.grad for n, t in p.items()}
+
+
+def _close(name, got, want, allowed):
+    got = got.double().cpu()
+    assert got.isfinite().all(), name
+    err = float((got - want).norm() / want.norm().clamp_min(1e-30))
+    assert err <= allowed, (name, err)
+
+
+@pytest.mark.parametrize("causal,activation,dtype", [(False, "gelu", torch.bfloat16), (True, "silu", torch.float16)])
+def test_training_step(causal, activation, dtype):
+    layer = _layer(causal=causal, activation=activation, dtype=dtype)
+    gen = torch.Generator().manual_seed(1)
+    x, dy = (torch.randn(3, 75, 128, generator=gen).to(dtype) for _ in range(2))
+    lens = [75, 33, 60]
+    y = layer.forward(x.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda:0"))
+    dx = layer.backward(dy.cuda())
+    torch.cuda.synchronize()
+    wy, wx, wg = _reference(layer, x, lens, dy)
+    # About ten roundings (relative deviation 2^-8/sqrt 3 or 2^-11/sqrt 3 each, independent) lie between an
+    # input and a gradient: sqrt 10 of them, and as much again for what the products amplify.
+    allowed = 2 * 10 ** 0.5 * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11) / 3 ** 0.5
+    _close("y", y, wy, allowed)
+    _close("dx", dx, wx, allowed)
+    for n, g in layer.grads.items():
+        if n == "bk":  # adding a vector to all keys changes no probability: the gradient is a rounding
+            assert float(g.abs().max()) <= allowed * float(wg["bq"].abs().max()) * 4
+            continue
+        _close(n, g, wg[n], 2 * allowed)
+
+
+def test_decoding_matches_the_training_forward():
+    layer = _layer(causal=True)
+    x = torch.randn(2, 40, 128, generator=torch.Generator().manual_seed(2)).to(layer.dtype).cuda()
+    want = layer.forward(x).clone()
+    cache = layer.new_cache(2, 64)
+    # a prompt of 30 tokens as one chunk, then token by token
+    lens = torch.full((2,), 30, dtype=torch.int32, device="cuda:0")
+    got = [layer.decode(x[:, :30].contiguous(), cache, torch.arange(30, device="cuda:0").expand(2, -1), lens).clone()]
+    for t in range(30, 40):
+        lens = torch.full((2,), t + 1, dtype=torch.int32, device="cuda:0")
+        got.append(layer.decode(x[:, t:t + 1].contiguous(), cache, torch.full((2, 1), t, device="cuda:0"), lens).clone())
+    torch.cuda.synchronize()
+    err = (torch.cat(got, 1).double() - want.double()).norm() / want.double().norm()
+    assert float(err) <= 4 * 2.0 ** -8 / 3 ** 0.5, float(err)
+
+
+def test_graph_replays_give_the_eager_results():
+    """Forward and backward captured on a side stream; every replay, with eager work between them,
+    gives the eager call's bits for the inputs of that replay."""
+    layer = _layer(causal=True)
+    stream = torch.cuda.Stream()
+    shape = (2, 70, 128)
+    x, dy = (torch.zeros(shape, dtype=layer.dtype, device="cuda:0") for _ in range(2))
+    lens = torch.tensor([70, 41], dtype=torch.int32, device="cuda:0")
+    inputs = [[torch.randn(shape, generator=torch.Generator().manual_seed(s)).to(layer.dtype).cuda() for s in (i, 50 + i)]
+              for i in range(4)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        layer.forward(x, lens, stream=stream.cuda_stream)  # (buffers are made outside the graph)
+        layer.backward(dy, stream=stream.cuda_stream)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        y = layer.forward(x, lens, stream=stream.cuda_stream)
+        dx = layer.backward(dy, stream=stream.cuda_stream)
+    for a, b in inputs:
+        x.copy_(a)
+        dy.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [y.clone(), dx.clone()] + [layer.grads[n].clone() for n in sorted(layer.grads)]
+        eager_y = layer.forward(x, lens)
+        eager_dx = layer.backward(dy)
+        torch.cuda.synchronize()
+        for r, e in zip(replayed, [eager_y, eager_dx] + [layer.grads[n] for n in sorted(layer.grads)]):
+            assert torch.equal(r, e)
+
+
+def test_two_streams_at_once():
+    """Two layers on two streams of their own, with scratch of their own: the bits of one after the
+    other."""
+    layers = [_layer(causal=True, seed=s) for s in (1, 2)]
+    x = [torch.randn(2, 300, 128, generator=torch.Generator().manual_seed(s)).to(layers[0].dtype).cuda() for s in (3, 4)]
+    want = []
+    for layer, t in zip(layers, x):
+        y = layer.forward(t).clone()
+        want.append((y, layer.backward(t).clone()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    got = []
+    for layer, t, s in zip(layers, x, streams):
+        with torch.cuda.stream(s):
+            y = layer.forward(t, stream=s.cuda_stream)
+            got.append((y, layer.backward(t, stream=s.cuda_stream)))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
