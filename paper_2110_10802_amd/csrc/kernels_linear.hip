@@ -214,19 +214,22 @@ __device__ __forceinline__ void interleave()
     }
 }
 
+template <bool PX, bool QX, int TP, int TQ, int NBUF>
+constexpr int product_lds() { return NBUF * (Tile<PX, TP>::kBytes + Tile<QX, TQ>::kBytes); }
+
+// Workgroup `b` of part `part` of the contraction; lds: [NBUF][P tile, Q tile], 256-byte aligned
 template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF>
-__global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
+__device__ __forceinline__ void product_tile(const Product &a, char *lds, uint32_t b, int part)
 {
     constexpr int THREADS = WP * WQ * kWave, FP = TP / WP / 16, FQ = TQ / WQ / 16;
     typedef Tile<PX, TP> LP;
     typedef Tile<QX, TQ> LQ;
     constexpr int BUF = LP::kBytes + LQ::kBytes;
-    __shared__ __attribute__((aligned(256))) char lds[NBUF * BUF]; // [NBUF][P tile, Q tile]
     const uint32_t np = (a.np + TP - 1) / TP, nq = (a.nq + TQ - 1) / TQ;
     uint32_t tp, tq;
-    tile_of(blockIdx.x, np * nq, np, nq, tp, tq);
+    tile_of(b, np * nq, np, nq, tp, tq);
     const int p0 = tp * TP, q0 = tq * TQ;
-    const int c0 = blockIdx.y * a.steps * kStep, left = min(a.nc - c0, a.steps * kStep);
+    const int c0 = part * a.steps * kStep, left = min(a.nc - c0, a.steps * kStep);
     Loader<PX, TP, THREADS> lp;
     Loader<QX, TQ, THREADS> lq;
     lp.init(a.p, a.ldp, p0, a.np, c0);
@@ -314,11 +317,68 @@ __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
             if (q >= a.nq || p >= a.np)
                 continue;
             if (a.partial)
-                store8(a.partial + ((size_t)blockIdx.y * a.nq + q) * a.np + p, e);
+                store8(a.partial + ((size_t)part * a.nq + q) * a.np + p, e);
             else
                 finish<T>(a, q, p, e, bias);
         }
     }
+}
+
+template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF>
+__global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
+{
+    __shared__ __attribute__((aligned(256))) char lds[product_lds<PX, QX, TP, TQ, NBUF>()];
+    product_tile<T, PX, QX, TP, TQ, WP, WQ, NBUF>(a, lds, blockIdx.x, blockIdx.y);
+}
+
+// out[c] = sum over rows of in[rows][n]: a workgroup per 64 columns, its WAVES wavefronts take every
+// WAVES-th row.
+struct Columns {
+    const float *in;
+    int rows, n;
+    float *out;
+};
+template <int WAVES>
+__device__ __forceinline__ void column_sum(const Columns &a, int block, float (*red)[kWave])
+{
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, c = block * kWave + lane;
+    float s = 0.f;
+    if (c < a.n) {
+#pragma unroll 4
+        for (int r = w; r < a.rows; r += WAVES)
+            s += a.in[(size_t)r * a.n + c];
+    }
+    red[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && c < a.n) {
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v)
+            s += red[v][lane];
+        a.out[c] = s;
+    }
+}
+__global__ __launch_bounds__(1024) void column_sum_kernel(Columns a)
+{
+    __shared__ float red[16][kWave];
+    column_sum<16>(a, blockIdx.x, red);
+}
+
+// Both products of a backward pass in one launch, two workgroups to a CU: what one of them waits for, the
+// other multiplies through (4096 x 4096 x 1024: 42 + 42 us apart, 68 here).  `x` has tiles_x tiles in parts_x parts, `w` likewise;
+// the longer workgroups come first.  The last workgroups add up the partial rows of db, a launch less.
+template <class T>
+__global__ __launch_bounds__(512) void product_both_kernel(Product x, Product w, uint32_t tiles_x, uint32_t all_x,
+                                                           uint32_t tiles_w, uint32_t all_w, Columns db)
+{
+    __shared__ __attribute__((aligned(256))) char lds[product_lds<true, true, 128, 128, 2>()];
+    const bool x_first = x.steps >= w.steps;
+    const uint32_t b = blockIdx.x, first = x_first ? all_x : all_w, r = b < first ? b : b - first;
+    if (b >= all_x + all_w)
+        column_sum<8>(db, b - all_x - all_w, (float(*)[kWave])lds);
+    else if ((b < first) == x_first)
+        product_tile<T, true, false, 128, 128, 2, 4, 2>(x, lds, r % tiles_x, r / tiles_x);
+    else
+        product_tile<T, true, true, 128, 128, 2, 4, 2>(w, lds, r % tiles_w, r / tiles_w);
 }
 
 // The sum over the splits of a contraction, and the epilogue.
@@ -450,35 +510,17 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64
             psum[(size_t)blockIdx.y * n + c + i] = (red[0][i][lane] + red[1][i][lane]) + (red[2][i][lane] + red[3][i][lane]);
 }
 
-// out[c] = sum over rows of in[rows][n]: a workgroup per 64 columns, its sixteen wavefronts take every
-// sixteenth row.
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float *in, int rows, int n, float *out)
-{
-    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
-    __shared__ float red[16][kWave];
-    float s = 0.f;
-    if (c < n) {
-#pragma unroll 4
-        for (int r = w; r < rows; r += 16)
-            s += in[(size_t)r * n + c];
-    }
-    red[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && c < n) {
-#pragma unroll
-        for (int v = 1; v < 16; ++v)
-            s += red[v][lane];
-        out[c] = s;
-    }
-}
-
 constexpr int kCUs = 256;
 
 // Tile and split of a contraction.
 enum { ROWS16, ROWS32, TILE256, TILE128, TILE128_PAIR, TILE64 };
 struct Plan {
     int form, splits, steps; // steps per split
+    double time;             // us, as estimated
 };
+
+// us for the parts of a contraction: their way to memory and back, and the launch
+double adding_up(int np, int nq, int parts) { return parts > 1 ? 3 + 2e-6 * np * nq * parts : 0; }
 
 // px, qx: the operand lies across
 Plan plan_product(int np, int nq, int nc, bool px, bool qx)
@@ -489,16 +531,17 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
     // 16.2 / 13.5, 1 x 65536 x 1024 32.5 / 24.1, 32 x 4096 x 2048 8.1 / 12.1, 32 x 8192 x 8192 45 / 26).
     const int64_t weights = (int64_t)np * nc;
     if (!px && !qx && nq <= 16 && weights <= 1 << 24 && nc <= 6144)
-        return {ROWS16, 1, steps};
+        return {ROWS16, 1, steps, 0};
     if (!px && !qx && nq <= 32 && weights <= 1 << 23 && nc <= 4096)
-        return {ROWS32, 1, steps};
+        return {ROWS32, 1, steps, 0};
     // Up to 64 rows: six buffers of a 128 x 64 tile, 100 KB on the way to each CU (24 x 4096 x 16384 from
     // memory: 38.4 us, 42.7 with 128 x 128)
     if (!qx && nq <= 64) {
-        Plan p = {TILE64, 1, steps};
+        Plan p = {TILE64, 1, steps, 0};
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / ((np + 127) / 128), steps / 16));
         p.steps = std::max(1, (steps + p.splits - 1) / p.splits);
         p.splits = std::max(1, (steps + p.steps - 1) / p.steps);
+        p.time = std::max(0.3 * p.steps, (double)weights / 2.2e6) + adding_up(np, nq, p.splits);
         return p;
     }
     const int64_t t256 = (int64_t)((np + 255) / 256) * ((nq + 255) / 256);
@@ -508,7 +551,7 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
     // 1.0.
     const double big = 1.5 * (double)((t256 + kCUs - 1) / kCUs), one = 0.49 * (double)((t128 + kCUs - 1) / kCUs),
                  pair = std::max(1.0, (double)t128 / (2 * kCUs) + 0.3);
-    Plan p = {TILE256, 1, steps};
+    Plan p = {TILE256, 1, steps, big * steps};
     if (one <= big && one <= pair) {
         p.form = TILE128;
         // idle CUs take parts of the contraction, no shorter than 16 steps: adding the parts up costs a
@@ -516,9 +559,17 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / std::max<int64_t>(t128, 1), steps / 16));
         p.steps = std::max(1, (steps + p.splits - 1) / p.splits);
         p.splits = std::max(1, (steps + p.steps - 1) / p.steps);
+        p.time = one * p.steps + adding_up(np, nq, p.splits);
     } else if (pair < big)
-        p.form = TILE128_PAIR;
+        p.form = TILE128_PAIR, p.time = pair * steps;
     return p;
+}
+
+template <class T>
+void launch_finish(const Product &a, int splits, hipStream_t st)
+{
+    const size_t units = (size_t)a.nq * (a.np / 8);
+    product_finish_kernel<T><<<(unsigned)std::min<size_t>((units + 255) / 256, 4096), 256, 0, st>>>(a, splits);
 }
 
 template <class T, bool PX, bool QX>
@@ -550,10 +601,8 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
     default:
         product_kernel<T, PX, QX, 128, 128, 2, 4, 2><<<grid, 512, 0, st>>>(a);
     }
-    if (p.splits > 1) {
-        const size_t units = (size_t)a.nq * (a.np / 8);
-        product_finish_kernel<T><<<(unsigned)std::min<size_t>((units + 255) / 256, 4096), 256, 0, st>>>(a, p.splits);
-    }
+    if (p.splits > 1)
+        launch_finish<T>(a, p.splits, st);
     return hipGetLastError();
 }
 
@@ -561,6 +610,75 @@ size_t product_scratch(int np, int nq, int nc, bool px, bool qx)
 {
     const int s = plan_product(np, nq, nc, px, qx).splits;
     return s > 1 ? (size_t)s * np * nq * 4 : 0;
+}
+
+// Steps until workgroups of two lengths, the longer ones first, have left the places of two per CU.
+double packed(int64_t n1, int len1, int64_t n2, int len2)
+{
+    if (len1 < len2)
+        std::swap(n1, n2), std::swap(len1, len2);
+    const int64_t places = 2 * kCUs, late = n1 % places; // places that are one round of long ones behind
+    double a = (double)(n1 / places) * len1, b = late ? a + len1 : a;
+    const int64_t rounds = std::max<int64_t>(0, n2 / places - 4 - len1 / len2); // (whole rounds from the start)
+    n2 -= rounds * places;
+    double end = b;
+    while (n2 > 0) { // on the places that are free first
+        const bool on_a = a <= b || !late;
+        double &t = on_a ? a : b;
+        t += len2;
+        n2 -= on_a ? places - late : late;
+        end = std::max(end, t);
+    }
+    return end + (double)rounds * len2;
+}
+
+// Both products of a backward pass in one launch of 128 x 128 tiles?
+struct Both {
+    bool taken;
+    uint32_t tiles_x, tiles_w;
+    int steps_x, steps_w, parts_x, parts_w; // steps of a part
+    size_t partial_w, total;                // scratch: where the weight gradient's parts begin, all of it
+};
+Both plan_both(const dnnseq_linear_desc &d)
+{
+    Both b = {};
+    if (!d.m)
+        return b;
+    const auto tiles = [](int v) { return (v + 127) / 128; };
+    b.tiles_x = tiles(d.k) * tiles(d.m), b.tiles_w = tiles(d.k) * tiles(d.n);
+    const int sx = (d.n + kStep - 1) / kStep, sw = (d.m + kStep - 1) / kStep;
+    // no part much longer than what every place would have
+    const double each = ((double)b.tiles_x * sx + (double)b.tiles_w * sw) / (2 * kCUs);
+    const auto part = [&](int steps, int &parts, int &len) {
+        parts = std::max(1, std::min((int)(steps / std::max(each, 8.0) + 0.5), steps / 8));
+        len = (steps + parts - 1) / parts;
+        parts = (steps + len - 1) / len;
+    };
+    part(sx, b.parts_x, b.steps_x);
+    part(sw, b.parts_w, b.steps_w);
+    b.partial_w = b.parts_x > 1 ? (size_t)b.parts_x * d.k * d.m * 4 : 0;
+    b.total = b.partial_w + (b.parts_w > 1 ? (size_t)b.parts_w * d.k * d.n * 4 : 0);
+    const double t = 6 + 1.05 * packed((int64_t)b.tiles_x * b.parts_x, b.steps_x, (int64_t)b.tiles_w * b.parts_w, b.steps_w) +
+                     adding_up(d.k, d.m, b.parts_x) + adding_up(d.k, d.n, b.parts_w);
+    const Plan x = plan_product(d.k, d.m, d.n, true, false), w = plan_product(d.k, d.n, d.m, true, true);
+    b.taken = t < x.time + w.time + 16;
+    return b;
+}
+
+template <class T>
+hipError_t launch_both(Product x, Product w, const Columns &db, const Both &b, float *scratch, hipStream_t st)
+{
+    x.steps = b.steps_x, w.steps = b.steps_w;
+    x.partial = b.parts_x > 1 ? scratch : nullptr;
+    w.partial = b.parts_w > 1 ? (float *)((char *)scratch + b.partial_w) : nullptr;
+    const uint32_t all_x = b.tiles_x * b.parts_x, all_w = b.tiles_w * b.parts_w;
+    const uint32_t sums = db.out ? (db.n + kWave - 1) / kWave : 0;
+    product_both_kernel<T><<<all_x + all_w + sums, 512, 0, st>>>(x, w, b.tiles_x, all_x, b.tiles_w, all_w, db);
+    if (b.parts_x > 1)
+        launch_finish<T>(x, b.parts_x, st);
+    if (b.parts_w > 1)
+        launch_finish<T>(w, b.parts_w, st);
+    return hipGetLastError();
 }
 
 size_t align(size_t v) { return (v + 255) / 256 * 256; }
@@ -587,7 +705,8 @@ BackwardScratch backward_layout(const dnnseq_linear_desc &d)
     s.g = 0;
     s.psum = d.activation ? align((size_t)d.m * d.n * 2) : 0;
     s.product = s.psum + align((size_t)((d.m + kGradRows - 1) / kGradRows) * d.n * 4);
-    s.total = s.product + std::max(product_scratch(d.k, d.m, d.n, true, false), product_scratch(d.k, d.n, d.m, true, true));
+    s.total = s.product + std::max({product_scratch(d.k, d.m, d.n, true, false), product_scratch(d.k, d.n, d.m, true, true),
+                                    plan_both(d).total});
     return s;
 }
 
@@ -626,25 +745,30 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
             ldg = d.n;
         }
     }
-    if (db)
-        column_sum_kernel<<<(d.n + kWave - 1) / kWave, 1024, 0, st>>>((const float *)(ws + l.psum), parts, d.n, db);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && dx && d.m) {
-        Product a = {};
-        a.p = w, a.ldp = d.ldw, a.np = d.k;
-        a.q = g, a.ldq = ldg, a.nq = d.m;
-        a.nc = d.n;
-        a.add = dx_add, a.ldadd = d.lddx_add, a.out = dx, a.ldo = d.lddx;
-        e = launch_product<T, true, false>(a, (float *)(ws + l.product), st);
+    const Columns sums = {(const float *)(ws + l.psum), parts, d.n, db};
+    Product px = {}, pw = {};
+    px.p = w, px.ldp = d.ldw, px.np = d.k;
+    px.q = g, px.ldq = ldg, px.nq = d.m;
+    px.nc = d.n;
+    px.add = dx_add, px.ldadd = d.lddx_add, px.out = dx, px.ldo = d.lddx;
+    pw.p = x, pw.ldp = d.ldx, pw.np = d.k;
+    pw.q = g, pw.ldq = ldg, pw.nq = d.n;
+    pw.nc = d.m;
+    pw.out = dw, pw.ldo = d.lddw, pw.out32 = d.dw_fp32;
+    if (e == hipSuccess && dx && dw) {
+        const Both both = plan_both(d);
+        if (both.taken)
+            return launch_both<T>(px, pw, sums, both, (float *)(ws + l.product), st);
     }
-    if (e == hipSuccess && dw) {
-        Product a = {};
-        a.p = x, a.ldp = d.ldx, a.np = d.k;
-        a.q = g, a.ldq = ldg, a.nq = d.n;
-        a.nc = d.m;
-        a.out = dw, a.ldo = d.lddw, a.out32 = d.dw_fp32;
-        e = launch_product<T, true, true>(a, (float *)(ws + l.product), st);
+    if (e == hipSuccess && db) {
+        column_sum_kernel<<<(d.n + kWave - 1) / kWave, 1024, 0, st>>>(sums);
+        e = hipGetLastError();
     }
+    if (e == hipSuccess && dx && d.m)
+        e = launch_product<T, true, false>(px, (float *)(ws + l.product), st);
+    if (e == hipSuccess && dw)
+        e = launch_product<T, true, true>(pw, (float *)(ws + l.product), st);
     return e;
 }
 

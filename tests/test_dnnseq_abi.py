@@ -264,3 +264,13 @@ def test_tolerances_catch_mistakes():
     x, w = torch.randn(9, 64, generator=gen).half(), torch.randn(16, 64, generator=gen).half()
     a, tol = ref.linear(x, w, torch.full((16,), 0.25))
     assert ((a["y"] - ref.linear(x, w)[0]["y"]).abs() > tol["y"]).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(0, 64, 64), (0, 4096, 8), (1, 8, 8), (1, 16384, 8), (7, 8, 16384), (1 << 24, 8, 8),
+                                   (65, 2056, 4104), (1 << 20, 4096, 64)])
+def test_linear_scratch_of_any_size(m, n, k):
+    """Sizes only: a number of bytes that is at least the rounded gradient's, and of its order."""
+    d = S.linear_desc(_t(1, k), _t(n, k), "gelu")
+    d.m = m
+    assert S.linear_forward_scratch_bytes(d) < 1 << 40
+    assert 2 * m * n <= S.linear_backward_scratch_bytes(d) < (64 << 20) + 80 * (m * n + m * k + n * k)

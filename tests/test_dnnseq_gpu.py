@@ -319,6 +319,44 @@ def test_linear_long_contractions(m, n, k):
     _linear(torch.bfloat16, m, n, k, "none", dw_fp32=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(1500, 520, 264), (130, 4104, 264), (1030, 1032, 264), (70, 2056, 520), (2049, 64, 72)])
+def test_linear_gradients_in_parts(dtype, m, n, k):
+    """Contractions that are long for one of the two gradients, or for both."""
+    _linear(TYPES[dtype], m, n, k, "silu", pad=8, dx_add=m > 1000, dw_fp32=m == 1030)
+
+
+@pytest.mark.parametrize("m,n,k", [(1000, 4096, 4104), (4100, 2056, 520), (2056, 1000, 4096)])
+def test_linear_gradients_together_and_alone(m, n, k):
+    """Larger gradients, asked for in one call and one by one; some of their rows against 64 bits."""
+    S = _S()
+    gen = _gen(m, n)
+    x, dy = torch.randn(m, k, generator=gen).bfloat16(), torch.randn(m, n, generator=gen).bfloat16()
+    w = (torch.randn(n, k, generator=gen) * k ** -0.5).bfloat16()
+    xd, wd, dyd = x.cuda(), w.cuda(), dy.cuda()
+    desc = S.linear_desc(xd, wd)
+    ws = _scratch(S.linear_backward_scratch_bytes(desc))
+    rows, cols = [0, 1, 127, 128, 255, 256, m // 2, m - 1], [0, 7, 127, 128, 257, n // 2, n - 2, n - 1]
+    want_x, tol_x = ref.linear_backward(x[rows], w, dy[rows])
+    want_w, tol_w = ref.linear_backward(x, w[cols], dy[:, cols])
+    for parts in ("xwb", "x", "w", "b", "xw"):
+        dx, dw = torch.full_like(xd, NAN), torch.full_like(wd, NAN)
+        db = torch.full((n,), NAN, device="cuda:0")
+        print(f"[dnnseq] gradients {parts} of {m} x {n} x {k}", flush=True)
+        S.linear_backward(desc, xd, wd, dyd, dx=dx if "x" in parts else None, dw=dw if "w" in parts else None,
+                          db=db if "b" in parts else None, scratch=ws)
+        torch.cuda.synchronize()
+        if "x" in parts:
+            ref.check("dx", dx[rows], want_x["dx"], tol_x["dx"])
+            assert dx.isfinite().all()
+        if "w" in parts:
+            ref.check("dw", dw[cols], want_w["dw"], tol_w["dw"])
+            assert dw.isfinite().all()
+        if "b" in parts:
+            ref.check("db", db[cols], want_w["db"], tol_w["db"])
+            assert db.isfinite().all()
+
+
 def test_linear_in_place_residuals_and_parts():
     """y over the residual, dx over dx_add, and calls that ask for one gradient only."""
     S = _S()
