@@ -167,13 +167,66 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(const u
     }
 }
 
+// dgamma and dbeta of kCols columns in full: groups of as many lanes take every row of their number, eight
+// rows on the way at a time; their sums are added in order.
+constexpr int kCols = 32;
+struct Columns {
+    const uint16_t *x, *dy;
+    int64_t ldx, lddy;
+    const float *mean, *rstd;
+    int rows, cols;
+    float *dgamma, *dbeta; // NULL: the rows' workgroups leave partial sums
+};
+template <class T, int THREADS>
+__device__ __forceinline__ void norm_columns(const Columns &a, int block)
+{
+    constexpr int GROUPS = THREADS / kCols;
+    __shared__ float red[2][GROUPS][kCols];
+    const int g = threadIdx.x / kCols, i = threadIdx.x % kCols, c = block * kCols + i, at = min(c, a.cols - 1);
+    float sg = 0.f, sb = 0.f;
+    for (int r0 = g; r0 < a.rows; r0 += 8 * GROUPS) {
+        uint16_t x[8], d[8];
+        float mu[8], rs[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t r = min(r0 + u * GROUPS, a.rows - 1);
+            x[u] = a.x[r * a.ldx + at];
+            d[u] = a.dy[r * a.lddy + at];
+            mu[u] = a.mean[r];
+            rs[u] = a.rstd[r];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (r0 + u * GROUPS >= a.rows)
+                break;
+            const float v = T::lo(d[u]);
+            sg = fmaf(v, (T::lo(x[u]) - mu[u]) * rs[u], sg);
+            sb += v;
+        }
+    }
+    red[0][g][i] = sg;
+    red[1][g][i] = sb;
+    __syncthreads();
+    if (g < 2 && c < a.cols) {
+        float s = red[g][0][i];
+#pragma unroll
+        for (int j = 1; j < GROUPS; ++j)
+            s += red[g][j][i];
+        (g ? a.dbeta : a.dgamma)[c] = s;
+    }
+}
+
 template <class T, int TPR, int NU, bool ADD>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
     const uint16_t *x, int64_t ldx, const uint16_t *dy, int64_t lddy, const float *gamma, const float *mean,
     const float *rstd, const uint16_t *add, int64_t ldadd, int rows, int cols, uint16_t *dx, int64_t lddx,
-    float *pgamma, float *pbeta)
+    float *pgamma, float *pbeta, int groups, float *dgamma, float *dbeta)
 {
     constexpr int THREADS = TPR > 256 ? TPR : 256, G = THREADS / TPR, W = TPR / kWave;
+    if ((int)blockIdx.x >= groups) {
+        norm_columns<T, THREADS>({x, dy, ldx, lddy, mean, rstd, rows, cols, dgamma, dbeta}, blockIdx.x - groups);
+        return;
+    }
     __shared__ float red[2][W > 1 ? 2 * W : 1];
     const int t = threadIdx.x % TPR;
     float g[NU][8], ag[NU][8], ab[NU][8];
@@ -185,7 +238,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
             ag[u][i] = ab[u][i] = 0.f;
     }
     const float inv = 1.0f / (float)cols;
-    const int first = blockIdx.x * G + threadIdx.x / TPR, step = gridDim.x * G;
+    const int first = blockIdx.x * G + threadIdx.x / TPR, step = groups * G;
     Units<NU> nx, nd, na;
     const auto fetch = [&](int r) __attribute__((always_inline)) {
         nx.template load<TPR>(x + r * ldx, cols, t);
@@ -247,6 +300,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
             store_unit<T>(dx + r * lddx, cols, (u * TPR + t) * 8, f);
         }
     }
+    if (dgamma)
+        return;
     // one partial row per workgroup, its thread groups added in a fixed order
     __shared__ float part[G > 1 ? G : 1][G > 1 ? TPR * NU * 8 : 1];
 #pragma unroll
@@ -322,11 +377,19 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float *pgamma, con
 
 int rows_per_group(int cols) { return cols <= 128 ? 16 : cols <= 1024 ? 4 : 1; }
 
+// Workgroups, and so partial rows: more of them hide the latency of few rows each, and cost 16 bytes per
+// column on their way to memory and back (rows x columns, us with 128 / 256 / 512: 512 x 4096 14.5 / 16.1 / 24.3,
+// 2048 x 4096 32.4 / 24.3 / 26.4, 8192 x 2048 74 / 42 / 31; rows past 4096 columns have one workgroup a CU).
 int backward_groups(const dnnseq_layernorm_desc &d)
 {
-    const int per = rows_per_group(d.cols);
-    return std::min((d.rows + per - 1) / per, d.cols <= 4096 ? 512 : 256);
+    const int per = rows_per_group(d.cols), fill = std::max({128, std::min(d.rows / 4, 256), d.rows / 8});
+    return std::min({(d.rows + per - 1) / per, fill, d.cols <= 4096 ? 512 : 256});
 }
+
+// Few rows: workgroups beside the rows' read x and dy a second time for the columns' sums, a launch less
+// (rows x columns, direct / in parts: 77 x 1001 5.1 / 8.1 us, 192 x 2048 8.3 / 9.2, 256 x 2048 12.9 / 8.5, 512 x 8192
+// 13.8 / 21.1, 1024 x 8192 25.5 / 27.0).
+bool direct_columns(const dnnseq_layernorm_desc &d) { return d.rows > 0 && d.rows <= (d.cols <= 4096 ? 192 : 512); }
 
 template <class T>
 void forward(const dnnseq_layernorm_desc &d, const void *x, const float *gamma, const float *beta, void *y,
@@ -343,12 +406,15 @@ void forward(const dnnseq_layernorm_desc &d, const void *x, const float *gamma, 
 
 template <class T, bool ADD>
 void backward(const dnnseq_layernorm_desc &d, const void *x, const void *dy, const float *gamma, const float *mean,
-              const float *rstd, const void *add, void *dx, float *pgamma, float *pbeta, int grid, hipStream_t st)
+              const float *rstd, const void *add, void *dx, float *pgamma, float *pbeta, int groups, float *dgamma,
+              float *dbeta, hipStream_t st)
 {
+    const int grid = groups + (dgamma ? (d.cols + kCols - 1) / kCols : 0);
 #define NORM_BWD(TPR, NU)                                                                                              \
     norm_bwd_kernel<T, TPR, NU, ADD><<<grid, TPR > 256 ? TPR : 256, 0, st>>>(                                          \
         (const uint16_t *)x, d.ldx, (const uint16_t *)dy, d.lddy, gamma, mean, rstd, (const uint16_t *)add,            \
-        d.lddx_add, d.rows, d.cols, (uint16_t *)dx, d.lddx, pgamma, pbeta)
+        d.lddx_add, d.rows, d.cols, (uint16_t *)dx, d.lddx, pgamma, pbeta, groups, dgamma,    \
+        dbeta)
     NORM_FORMS(NORM_BWD);
 #undef NORM_BWD
 }
@@ -372,12 +438,15 @@ hipError_t launch_norm_backward(const dnnseq_layernorm_desc &d, const void *x, c
                                 float *dbeta, void *scratch, hipStream_t st)
 {
     const int grid = backward_groups(d);
+    const bool direct = direct_columns(d);
     float *pgamma = (float *)scratch, *pbeta = pgamma + (size_t)grid * d.cols;
     const auto f = d.dtype == DNNSEQ_FP16 ? (dx_add ? backward<FP16, true> : backward<FP16, false>)
                                           : (dx_add ? backward<BF16, true> : backward<BF16, false>);
     if (d.rows)
-        f(d, x, dy, gamma, mean, rstd, dx_add, dx, pgamma, pbeta, grid, st);
-    norm_sum_kernel<<<dim3((d.cols + kWave - 1) / kWave, 2), 1024, 0, st>>>(pgamma, pbeta, grid, d.cols, dgamma, dbeta);
+        f(d, x, dy, gamma, mean, rstd, dx_add, dx, pgamma, pbeta, grid, direct ? dgamma : nullptr,
+          direct ? dbeta : nullptr, st);
+    if (!direct)
+        norm_sum_kernel<<<dim3((d.cols + kWave - 1) / kWave, 2), 1024, 0, st>>>(pgamma, pbeta, grid, d.cols, dgamma, dbeta);
     return hipGetLastError();
 }
 

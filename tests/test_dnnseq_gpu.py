@@ -466,6 +466,13 @@ def test_layernorm(dtype, rows, cols, add):
     assert torch.equal(dg, dg2) and torch.equal(db, db2)
 
 
+@pytest.mark.parametrize("rows,cols", [(193, 33), (192, 4095), (194, 1001), (512, 4104), (513, 4100), (1030, 520),
+                                       (31, 12001), (2100, 40)])
+def test_layernorm_column_sums(rows, cols):
+    """Few and many rows: sums of the columns in one pass and in parts."""
+    test_layernorm("bf16", rows, cols, rows % 2 == 0)
+
+
 def test_layernorm_rows_far_from_zero_and_no_rows():
     """A mean a thousand times the deviation (the variance is taken about the mean), and no rows."""
     S = _S()
