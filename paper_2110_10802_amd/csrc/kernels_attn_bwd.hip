@@ -46,10 +46,21 @@ __device__ __forceinline__ int64_t row_offset(const dnnseq_stride &s, int b, int
     return b * s.batch + head * s.head + token * s.token;
 }
 
-// A workgroup per 64 rows, 16 lanes to a row; rows of dout first (delta and norm), then, for fp16, rows of
-// v (norm).
+// Eight products' sum.
 template <class T>
-__global__ __launch_bounds__(256) void attn_delta_kernel(Backward a)
+__device__ __forceinline__ float dot8(const u32x4 &x, const u32x4 &y)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        s += T::lo(x[j]) * T::lo(y[j]) + T::hi(x[j]) * T::hi(y[j]);
+    return s;
+}
+
+// fp16: the largest square of a row's norm.  A workgroup per 64 rows, 16 lanes to a row; rows of dout
+// first, then rows of v.
+template <class T>
+__global__ __launch_bounds__(256) void attn_norm_kernel(Backward a)
 {
     const int lane = threadIdx.x % 16, c = lane * 8;
     const bool of_v = (int)blockIdx.x >= a.bounds_q;
@@ -57,51 +68,30 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(Backward a)
     const int item = blockIdx.x - (of_v ? a.bounds_q : 0), tiles = (len + kTileRows - 1) / kTileRows;
     const int bh = item / tiles, t0 = item % tiles * kTileRows + threadIdx.x / 16, h = bh % heads, b = bh / heads;
     const int top = clamp_len(of_v ? a.kv_lens : a.q_lens, b, len);
-    u32x4 x[4], y[4];
+    u32x4 x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int t = t0 + 16 * i;
-        x[i] = y[i] = u32x4{0, 0, 0, 0};
-        if (t < top && c < a.dim) {
+        x[i] = u32x4{0, 0, 0, 0};
+        if (t < top && c < a.dim)
             x[i] = *(const u32x4 *)((of_v ? a.v + row_offset(a.sv, b, h, t) : a.dout + row_offset(a.sdo, b, h, t)) + c);
-            if (!of_v)
-                y[i] = *(const u32x4 *)(a.o + row_offset(a.so, b, h, t) + c);
-        }
     }
     float largest = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float dot = 0.f, norm = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            dot += T::lo(x[i][j]) * T::lo(y[i][j]) + T::hi(x[i][j]) * T::hi(y[i][j]);
-            norm += T::lo(x[i][j]) * T::lo(x[i][j]) + T::hi(x[i][j]) * T::hi(x[i][j]);
-        }
-        dot = mbk::row16_sum(dot);
-        const int t = t0 + 16 * i;
-        if (!of_v && lane == 0) {
-            const size_t at = (size_t)bh * a.q_pad + t;
-            const float l = t < top ? a.lse[(size_t)bh * len + t] : -INFINITY;
-            a.minus[at] = -dot;
-            a.lse2[at] = l == -INFINITY ? INFINITY : l * kLog2e;
-        }
-        if (T::kHalf)
-            largest = fmaxf(largest, mbk::row16_sum(norm));
-    }
-    if (T::kHalf) {
-        __shared__ float red[16];
-        if (lane == 0)
-            red[threadIdx.x / 16] = largest;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int i = 1; i < 16; ++i)
-                largest = fmaxf(largest, red[i]);
-            a.bound[blockIdx.x] = largest;
-        }
+    for (int i = 0; i < 4; ++i)
+        largest = fmaxf(largest, mbk::row16_sum(dot8<T>(x[i], x[i])));
+    __shared__ float red[16];
+    if (lane == 0)
+        red[threadIdx.x / 16] = largest;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i)
+            largest = fmaxf(largest, red[i]);
+        a.bound[blockIdx.x] = largest;
     }
 }
 
-// The maxima over the workgroups of attn_delta, one number each.
+// The maxima over the workgroups of attn_norm, one number each.
 __global__ __launch_bounds__(1024) void attn_bound_kernel(Backward a)
 {
     const int n = blockIdx.x ? a.bounds_v : a.bounds_q;
@@ -452,13 +442,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
     const int head = g * a.group + r % a.group, token = r / a.group;
     const bool in = r < rows && token < ql;
     const uint16_t *qrow = a.q + row_offset(a.sq, b, head, token), *drow = a.dout + row_offset(a.sdo, b, head, token);
+    const uint16_t *orow = a.o + row_offset(a.so, b, head, token);
+    const float lse = in ? a.lse[((size_t)b * a.q_heads + head) * a.q_len + token] : -INFINITY;
+    float delta = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * NS; ++i) {
         q[i] = own_fragment(qrow, in, a.dim, i);
         d[i] = own_fragment(drow, in, a.dim, i);
+        delta += dot8<T>(d[i], own_fragment(orow, in, a.dim, i));
     }
-    const size_t ri = ((size_t)b * a.q_heads + head) * a.q_pad + token;
-    const float lse2 = in ? a.lse2[ri] : INFINITY, minus = in ? a.minus[ri] : 0.f;
+    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e, minus = -halves_sum(delta);
     float rest = 0.f;
     Load lk, lv;
     lk.init(a.k + row_offset(a.sk, b, g, 0), a.sk.token, a.dim);
@@ -523,8 +516,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
         __builtin_amdgcn_s_waitcnt(0x0f70); // (no load into LDS may outlive the workgroup)
     }
     rest = halves_sum(rest);
-    if (in && lane < 32)
+    if (r < rows && lane < 32) {
+        const size_t ri = ((size_t)b * a.q_heads + head) * a.q_pad + token;
         a.minus[ri] = minus - rest / c;
+        a.lse2[ri] = lse2;
+        if (token == a.q_len - 1) // the rest of the last tile of rows
+            for (int t = a.q_len; t < a.q_pad; ++t) {
+                a.minus[ri + t - token] = 0.f;
+                a.lse2[ri + t - token] = INFINITY;
+            }
+    }
     if (r < rows)
         store_row<T, NS>(a.dq + row_offset(a.sdq, b, head, token), dq, a.dim, a.scale / c);
 }
@@ -558,10 +559,9 @@ Layout layout(const dnnseq_attention_desc &d)
 template <class T, int NS>
 hipError_t backward(const Backward &a, hipStream_t st)
 {
-    if (a.bounds_q + a.bounds_v) {
-        attn_delta_kernel<T><<<a.bounds_q + a.bounds_v, 256, 0, st>>>(a);
-        if (T::kHalf)
-            attn_bound_kernel<<<2, 1024, 0, st>>>(a);
+    if (T::kHalf && a.bounds_q + a.bounds_v) {
+        attn_norm_kernel<T><<<a.bounds_q + a.bounds_v, 256, 0, st>>>(a);
+        attn_bound_kernel<<<2, 1024, 0, st>>>(a);
     }
     if (a.q_len)
         attn_dq_kernel<T, NS><<<grid_of(a.q_order), 256, 0, st>>>(a);
