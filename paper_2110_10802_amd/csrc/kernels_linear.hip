@@ -6,6 +6,13 @@
 // One kernel (dnnseq_gemm.h) serves the three: only the loaders and fragment readers differ.  g is
 // written once by an elementwise pass that also sums db, in the type of the tensors: the matrix
 // cores take 16-bit operands, so it is rounded where any of its uses would round it.
+//
+// What bounds it: 8192 x 8192 x 8192 in tiles of 256 x 256, 770 us, 1.42 PFLOP/s: the matrix units are busy for 74 %
+// of the cycles at 1.83 GHz, the rest goes to the barrier of each step and to the operands' first reads behind it.
+// Short contractions add the epilogue, which nothing overlaps with one tile to a CU (4096 x 4096 x 1024 with GELU and z
+// kept: 41.5 us, 24 of them the steps, 67 MB of results).  Up to 64 rows: reading the weights (24 x 4096 x
+// 16384 39 us, 3.5 TB/s).  One row: a launch and the workgroups' first reads (1 x 4096 x 1024 4.7 us).
+// act_grad: memory, 100 MB in 20 us, 5 TB/s.
 #include "dnnseq_gemm.h"
 #include "dnnseq_launch.h"
 
