@@ -51,6 +51,7 @@ bool disjoint(const dnnseq_stride &s, int64_t batch, int64_t heads, int64_t len,
 }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 40;      // times any 32-bit index within 63 bits
+constexpr int64_t kMaxHeads = 1 << 20, kMaxTokens = 1 << 28, kMaxGroups = 1 << 23;
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 22; // a tile's rows within 31 bits of bytes
 
 dnnseq_status check_attention(const dnnseq_attention_desc *d, bool backward)
@@ -69,8 +70,11 @@ dnnseq_status check_attention(const dnnseq_attention_desc *d, bool backward)
                      !disjoint(d->dk, d->batch, d->kv_heads, d->kv_len, d->head_dim) ||
                      !disjoint(d->dv, d->batch, d->kv_heads, d->kv_len, d->head_dim)))
         return DNNSEQ_EINVAL;
-    if (d->head_dim % 8 || d->head_dim > DNNSEQ_MAX_HEAD_DIM || d->q_len > (1 << 28) || d->kv_len > (1 << 28) ||
-        (int64_t)d->batch * d->q_heads > 65535)
+    // rows of a group and workgroups within 31 bits (a workgroup has 256 threads and takes 64 rows or more)
+    const int64_t heads = (int64_t)d->batch * d->q_heads, kv_heads = (int64_t)d->batch * d->kv_heads;
+    if (d->head_dim % 8 || d->head_dim > DNNSEQ_MAX_HEAD_DIM || heads > kMaxHeads || d->q_len > kMaxTokens ||
+        d->kv_len > kMaxTokens || (int64_t)d->q_len * (d->q_heads / d->kv_heads) > kMaxTokens ||
+        heads * (d->q_len / 64 + 1) > kMaxGroups || kv_heads * (d->kv_len / 64 + 1) > kMaxGroups)
         return DNNSEQ_EUNSUPPORTED;
     for (int i = 0; i < (backward ? 8 : 4); ++i)
         if (all[i]->batch > kMaxStride || all[i]->head > kMaxStride || all[i]->token >= kMaxTokenStride)

@@ -470,7 +470,8 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64
                                                        int64_t ldz, int m, int n, uint16_t *g, float *psum)
 {
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-    const int c = (blockIdx.x * kWave + lane) * 8, r0 = blockIdx.y * kGradRows + w * (kGradRows / 4);
+    const uint32_t blocks = (n + 8 * kWave - 1) / (8 * kWave), part = blockIdx.x / blocks; // (a grid's second dimension is short)
+    const int c = ((blockIdx.x - part * blocks) * kWave + lane) * 8, r0 = part * kGradRows + w * (kGradRows / 4);
     const int r1 = min(r0 + kGradRows / 4, m);
     __shared__ float red[4][8][kWave];
     Eight s = {};
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64
 #pragma unroll
     for (int i = threadIdx.x / kWave; i < 8; i += 4)
         if (c < n)
-            psum[(size_t)blockIdx.y * n + c + i] = (red[0][i][lane] + red[1][i][lane]) + (red[2][i][lane] + red[3][i][lane]);
+            psum[(size_t)part * n + c + i] = (red[0][i][lane] + red[1][i][lane]) + (red[2][i][lane] + red[3][i][lane]);
 }
 
 constexpr int kCUs = 256;
@@ -727,7 +728,7 @@ hipError_t backward(const dnnseq_linear_desc &d, const void *x, const void *w, c
     int64_t ldg = d.lddy;
     const int parts = (d.m + kGradRows - 1) / kGradRows;
     if ((d.activation || db) && d.m) {
-        const dim3 grid((d.n + 511) / 512, parts);
+        const unsigned grid = (unsigned)((d.n + 511) / 512) * parts;
         float *psum = db ? (float *)(ws + l.psum) : nullptr;
         const auto grad = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>((const uint16_t *)dy, d.lddy, (const uint16_t *)z, d.ldz, d.m, d.n,
                                         (uint16_t *)(ws + l.g), psum); };

@@ -274,3 +274,27 @@ def test_linear_scratch_of_any_size(m, n, k):
     d.m = m
     assert S.linear_forward_scratch_bytes(d) < 1 << 40
     assert 2 * m * n <= S.linear_backward_scratch_bytes(d) < (64 << 20) + 80 * (m * n + m * k + n * k)
+
+
+def _many(batch, q_heads, kv_heads, q_len, kv_len):
+    d = S.attention_desc(_t(1, q_heads, 1, 8), _t(1, kv_heads, 1, 8), _t(1, kv_heads, 1, 8), _t(1, q_heads, 1, 8))
+    d.batch, d.q_len, d.kv_len = batch, q_len, kv_len
+    for t, heads, length in (("q", q_heads, q_len), ("o", q_heads, q_len), ("dout", q_heads, q_len), ("dq", q_heads, q_len),
+                             ("k", kv_heads, kv_len), ("v", kv_heads, kv_len), ("dk", kv_heads, kv_len),
+                             ("dv", kv_heads, kv_len)):
+        s = getattr(d, t)
+        s.token, s.head, s.batch = 8, 8 * max(length, 1), 8 * max(length, 1) * heads
+    return d
+
+
+@pytest.mark.parametrize("sizes,taken", [
+    ((1 << 15, 32, 8, 1, 4096), False), ((1 << 15, 32, 1, 1, 4096), True), ((1 << 15, 33, 1, 1, 64), False),
+    ((3000, 32, 8, 1, 16384), True), ((1, 1, 1, 1 << 28, 1 << 28), True), ((1, 1, 1, (1 << 28) + 8, 8), False),
+    ((1, 2, 1, 1 << 28, 8), False), ((1, 2, 1, 1 << 27, 8), True), ((1 << 10, 1 << 10, 1, 64 * 8, 8), False)])
+def test_attention_sizes_fit_a_launch(sizes, taken):
+    """Descriptors at both sides of the limits: taken ones ask for scratch or a pointer, others are refused."""
+    d = _many(*sizes)
+    with pytest.raises(S.DnnSeqError) as e:
+        S.attention_backward(d, None, None, None, None, None, None, None, None, None, None)
+    assert e.value.status == (-1 if taken else -2)
+    assert (S.attention_backward_scratch_bytes(d) > 0) == taken

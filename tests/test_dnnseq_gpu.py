@@ -257,6 +257,30 @@ def test_attention_gradient_against_differences():
         assert abs(got - diff) <= float((tol[name] * way.abs()).sum()) + 1e-6 * float(way.abs().sum()), (name, got, diff)
 
 
+def test_attention_many_heads():
+    """More (request, head) pairs than 16 bits count."""
+    S, gen, dt = _S(), _gen(77), torch.bfloat16
+    B, H, G, L, D = 9000, 8, 2, 10, 8
+    q = torch.randn(B, H, 1, D, generator=gen).to(dt)
+    k, v = (torch.randn(B, G, L, D, generator=gen).to(dt) for _ in range(2))
+    dout = torch.randn(B, H, 1, D, generator=gen).to(dt)
+    qd, kd, vd, doutd = q.cuda(), k.cuda(), v.cuda(), dout.cuda()
+    o, dq, dk, dv = (torch.full_like(t, NAN) for t in (qd, qd, kd, vd))
+    lse = torch.empty(B, H, 1, device="cuda:0")
+    d = S.attention_desc(qd, kd, vd, o)
+    print("[dnnseq] attention of 72000 heads", flush=True)
+    S.attention_forward(d, qd, kd, vd, o, lse=lse, scratch=_scratch(S.attention_forward_scratch_bytes(d)))
+    S.attention_backward(d, qd, kd, vd, o, doutd, lse, dq, dk, dv, _scratch(S.attention_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    for t in (o, dq, dk, dv):
+        assert t.isfinite().all()
+    for b in (0, 8191, 8192, 8999):
+        p = torch.softmax(q[b].double() @ k[b].double().repeat_interleave(H // G, 0).transpose(1, 2) * D ** -0.5, -1)
+        want = p @ v[b].double().repeat_interleave(H // G, 0)
+        # p rounded to 2^-9 of itself, o to 2^-9
+        assert ((o[b].double().cpu() - want).abs() <= 2.0 ** -7 * (p @ v[b].double().abs().repeat_interleave(H // G, 0))).all()
+
+
 # ---- linear ------------------------------------------------------------------------------------
 
 def _rows(t, pad=0):
@@ -381,6 +405,26 @@ def test_linear_in_place_residuals_and_parts():
         db = torch.empty(n, device="cuda:0")
         S.linear_backward(desc, None, None, dyd, db=db, scratch=ws)
         ref.check("db", db, want["db"], tol["db"])
+
+
+def test_linear_backward_of_very_many_rows():
+    """More blocks of rows than a grid's second dimension holds (65535)."""
+    S = _S()
+    m, n, k = 64 * 65540 + 5, 8, 8
+    x = torch.ones(m, k, dtype=torch.bfloat16, device="cuda:0")
+    dy = torch.zeros(m, n, dtype=torch.bfloat16, device="cuda:0")
+    dy[::4096, 3] = 1
+    dy[-1, 5] = 2
+    w = torch.eye(8, dtype=torch.bfloat16, device="cuda:0")
+    d = S.linear_desc(x, w, "relu")
+    z = torch.ones_like(dy)
+    dx, db = torch.full_like(x, NAN), torch.full((n,), NAN, device="cuda:0")
+    print("[dnnseq] linear backward of 4194565 rows", flush=True)
+    S.linear_backward(d, x, w, dy, z=z, dx=dx, db=db, scratch=_scratch(S.linear_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    ones = (m + 4095) // 4096
+    assert db.tolist() == [0, 0, 0, ones, 0, 2, 0, 0]
+    assert torch.equal(dx, dy)
 
 
 def test_linear_without_rows():
