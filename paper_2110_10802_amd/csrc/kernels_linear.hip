@@ -120,16 +120,27 @@ __device__ __forceinline__ u32x4 round8(const Eight &e)
     return u32x4{T::pack(e.v[0], e.v[1]), T::pack(e.v[2], e.v[3]), T::pack(e.v[4], e.v[5]), T::pack(e.v[6], e.v[7])};
 }
 
+// STREAM: past the caches; the 256 x 256 tiles write results that an L2 does not hold (4096 x 4096 x 1024 with z
+// 44.7 -> 42.6 us, 16384 x 4096 x 1024 175 -> 166, a product that reads the result included 289 -> 283).
+template <bool STREAM>
+__device__ __forceinline__ void store16(u32x4 *p, u32x4 v)
+{
+    if (STREAM)
+        __builtin_nontemporal_store(v, p);
+    else
+        *p = v;
+}
+
 // Eight consecutive p of row q: z, activation, what is added, and the store.  `e` holds the products,
 // `bias` the bias there (or zeros).
-template <class T>
+template <class T, bool STREAM = false>
 __device__ __forceinline__ void finish(const Product &a, int64_t q, int p, Eight e, const Eight &bias)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         e.v[i] += bias.v[i];
     if (a.z)
-        *(u32x4 *)((uint16_t *)a.z + q * a.ldz + p) = round8<T>(e);
+        store16<STREAM>((u32x4 *)((uint16_t *)a.z + q * a.ldz + p), round8<T>(e));
     switch (a.act) { // (the same for the whole launch)
     case DNNSEQ_ACT_RELU:
 #pragma unroll
@@ -163,7 +174,7 @@ __device__ __forceinline__ void finish(const Product &a, int64_t q, int p, Eight
     if (a.out32)
         store8((float *)a.out + q * a.ldo + p, e);
     else
-        *(u32x4 *)((uint16_t *)a.out + q * a.ldo + p) = round8<T>(e);
+        store16<STREAM>((u32x4 *)((uint16_t *)a.out + q * a.ldo + p), round8<T>(e));
 }
 
 // Tiles in the order of workgroups: the eight XCDs (workgroup b runs on XCD b % 8) take runs of
@@ -326,7 +337,7 @@ __device__ __forceinline__ void product_tile(const Product &a, char *lds, uint32
             if (a.partial)
                 store8(a.partial + ((size_t)part * a.nq + q) * a.np + p, e);
             else
-                finish<T>(a, q, p, e, bias);
+                finish<T, TP == 256>(a, q, p, e, bias);
         }
     }
 }

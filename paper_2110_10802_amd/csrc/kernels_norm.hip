@@ -49,12 +49,15 @@ __device__ __forceinline__ float element(const u32x4 &v, int i)
     return i % 2 ? T::hi(v[i / 2]) : T::lo(v[i / 2]);
 }
 
-template <class T>
+template <class T, bool STREAM>
 __device__ __forceinline__ void store_unit(uint16_t *row, int cols, int c, const float (&f)[8])
 {
     const u32x4 v = {T::pack(f[0], f[1]), T::pack(f[2], f[3]), T::pack(f[4], f[5]), T::pack(f[6], f[7])};
     if (c + 8 <= cols) {
-        *(u32x4_any *)(row + c) = v;
+        if (STREAM)
+            __builtin_nontemporal_store(v, (u32x4_any *)(row + c));
+        else
+            *(u32x4_any *)(row + c) = v;
         return;
     }
 #pragma unroll
@@ -84,7 +87,7 @@ __device__ __forceinline__ float lane_sum(float v)
     return TPR == 16 ? mbk::row16_sum(v) : mbk::wave_sum(v);
 }
 
-template <class T, int TPR, int NU>
+template <class T, int TPR, int NU, bool STREAM>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(const uint16_t *x, int64_t ldx,
                                                                          const float *gamma, const float *beta,
                                                                          float eps, int rows, int cols, uint16_t *y,
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(const u
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 f[i] = fmaf(g[u][i], (element<T>(a.v[u], i) - mu) * rs, b[u][i]);
-            store_unit<T>(y + r * ldy, cols, (u * TPR + t) * 8, f);
+            store_unit<T, STREAM>(y + r * ldy, cols, (u * TPR + t) * 8, f);
         }
         if (t == 0) {
             mean[r] = mu;
@@ -218,7 +221,7 @@ __device__ __forceinline__ void norm_columns(const Columns &a, int block)
     }
 }
 
-template <class T, int TPR, int NU, bool ADD>
+template <class T, int TPR, int NU, bool ADD, bool STREAM>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
     const uint16_t *x, int64_t ldx, const uint16_t *dy, int64_t lddy, const float *gamma, const float *mean,
     const float *rstd, const uint16_t *add, int64_t ldadd, int rows, int cols, uint16_t *dx, int64_t lddx,
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(
                 if (ADD)
                     f[i] += element<T>(o.v[u], i);
             }
-            store_unit<T>(dx + r * lddx, cols, (u * TPR + t) * 8, f);
+            store_unit<T, STREAM>(dx + r * lddx, cols, (u * TPR + t) * 8, f);
         }
     }
     if (dgamma)
@@ -393,27 +396,32 @@ int backward_groups(const dnnseq_layernorm_desc &d)
 // 13.8 / 21.1, 1024 x 8192 25.5 / 27.0).
 bool direct_columns(const dnnseq_layernorm_desc &d) { return d.rows > 0 && d.rows <= (d.cols <= 4096 ? 192 : 512); }
 
-template <class T>
+// Results past the caches: from 16 MiB on what is read next is not in an L2 anyway, and what the other tensors
+// leave there stays (backward of 16384 x 4096 with dx_add in a trace 112 -> 95 us, forward of 8192 x 2048 17.5 -> 14.6, a forward pass that
+// reads the result included 33.2 -> 32.4; 4096 x 1024, 8 MiB: no difference).
+bool streamed(const dnnseq_layernorm_desc &d) { return (int64_t)d.rows * d.cols >= 8 << 20; }
+
+template <class T, bool STREAM>
 void forward(const dnnseq_layernorm_desc &d, const void *x, const float *gamma, const float *beta, void *y,
              float *mean, float *rstd, hipStream_t st)
 {
     const int per = rows_per_group(d.cols), grid = std::min((d.rows + per - 1) / per, 2048);
 #define NORM_FWD(TPR, NU)                                                                                              \
-    norm_fwd_kernel<T, TPR, NU><<<grid, TPR > 256 ? TPR : 256, 0, st>>>((const uint16_t *)x, d.ldx, gamma, beta,        \
+    norm_fwd_kernel<T, TPR, NU, STREAM><<<grid, TPR > 256 ? TPR : 256, 0, st>>>((const uint16_t *)x, d.ldx, gamma, beta,        \
                                                                         d.eps, d.rows, d.cols, (uint16_t *)y, d.ldy,   \
                                                                         mean, rstd)
     NORM_FORMS(NORM_FWD);
 #undef NORM_FWD
 }
 
-template <class T, bool ADD>
+template <class T, bool ADD, bool STREAM>
 void backward(const dnnseq_layernorm_desc &d, const void *x, const void *dy, const float *gamma, const float *mean,
               const float *rstd, const void *add, void *dx, float *pgamma, float *pbeta, int groups, float *dgamma,
               float *dbeta, hipStream_t st)
 {
     const int grid = groups + (dgamma ? (d.cols + kCols - 1) / kCols : 0);
 #define NORM_BWD(TPR, NU)                                                                                              \
-    norm_bwd_kernel<T, TPR, NU, ADD><<<grid, TPR > 256 ? TPR : 256, 0, st>>>(                                          \
+    norm_bwd_kernel<T, TPR, NU, ADD, STREAM><<<grid, TPR > 256 ? TPR : 256, 0, st>>>(                                          \
         (const uint16_t *)x, d.ldx, (const uint16_t *)dy, d.lddy, gamma, mean, rstd, (const uint16_t *)add,            \
         d.lddx_add, d.rows, d.cols, (uint16_t *)dx, d.lddx, pgamma, pbeta, groups, dgamma,    \
         dbeta)
@@ -431,7 +439,9 @@ size_t norm_backward_scratch(const dnnseq_layernorm_desc &d)
 hipError_t launch_norm_forward(const dnnseq_layernorm_desc &d, const void *x, const float *gamma, const float *beta,
                                void *y, float *mean, float *rstd, hipStream_t st)
 {
-    (d.dtype == DNNSEQ_FP16 ? forward<FP16> : forward<BF16>)(d, x, gamma, beta, y, mean, rstd, st);
+    const auto f = streamed(d) ? (d.dtype == DNNSEQ_FP16 ? forward<FP16, true> : forward<BF16, true>)
+                               : (d.dtype == DNNSEQ_FP16 ? forward<FP16, false> : forward<BF16, false>);
+    f(d, x, gamma, beta, y, mean, rstd, st);
     return hipGetLastError();
 }
 
@@ -442,8 +452,11 @@ hipError_t launch_norm_backward(const dnnseq_layernorm_desc &d, const void *x, c
     const int grid = backward_groups(d);
     const bool direct = direct_columns(d);
     float *pgamma = (float *)scratch, *pbeta = pgamma + (size_t)grid * d.cols;
-    const auto f = d.dtype == DNNSEQ_FP16 ? (dx_add ? backward<FP16, true> : backward<FP16, false>)
-                                          : (dx_add ? backward<BF16, true> : backward<BF16, false>);
+    const bool half = d.dtype == DNNSEQ_FP16;
+    const auto f = streamed(d) ? (half ? (dx_add ? backward<FP16, true, true> : backward<FP16, false, true>)
+                                       : (dx_add ? backward<BF16, true, true> : backward<BF16, false, true>))
+                               : (half ? (dx_add ? backward<FP16, true, false> : backward<FP16, false, false>)
+                                       : (dx_add ? backward<BF16, true, false> : backward<BF16, false, false>));
     if (d.rows)
         f(d, x, dy, gamma, mean, rstd, dx_add, dx, pgamma, pbeta, grid, direct ? dgamma : nullptr,
           direct ? dbeta : nullptr, st);
