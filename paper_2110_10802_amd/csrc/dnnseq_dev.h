@@ -78,6 +78,11 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, void *dst, ui
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)dst, 16, (int)voff, 0, 0, 0);
 }
+// The same for what nothing reads again: past the caches.
+__device__ __forceinline__ void load_lds_once(__amdgpu_buffer_rsrc_t r, void *dst, uint32_t voff)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)dst, 16, (int)voff, 0, 0, 2);
+}
 // Four 16-bit elements down a column: within 16 lanes, lane i names four elements of row i/4 at
 // columns 4 (i%4) and receives rows 0..3 of column i.
 __device__ __forceinline__ u32x2 read_tr(const uint16_t *p)

@@ -66,7 +66,9 @@ struct Loader {
                 off[i] = kNowhere;
         }
     }
-    // left: elements of the contraction from this step's start; none: no memory is read
+    // left: elements of the contraction from this step's start; none: no memory is read.  ONCE: no other
+    // workgroup reads the operand, it passes by the caches
+    template <bool ONCE>
     __device__ __forceinline__ void load(char *lds, int left)
     {
         const int rows = ACROSS ? min(left, kStep) : limit;
@@ -81,7 +83,10 @@ struct Loader {
                 const int unit = id % L::kUnits ^ L::swizzle(id / L::kUnits);
                 o = unit * 8 < left ? o : kNowhere;
             }
-            load_lds(r, lds + i * (THREADS * 16) + w0, o);
+            if (ONCE)
+                load_lds_once(r, lds + i * (THREADS * 16) + w0, o);
+            else
+                load_lds(r, lds + i * (THREADS * 16) + w0, o);
         }
         base += step;
     }

@@ -13,9 +13,10 @@
 //               SIMD hardly overlap them.  2 x 16 heads on 4 x 4093 x 128, causal: 145 us in a trace, 0.95
 //               PFLOP/s; 8 x 16 heads x 512 x 64, 205 to 512 tokens: 16 us
 //   attn_token  at most 16 rows (single tokens): bound by reading keys and values once; each wavefront
-//               walks its own chunks of 32 keys, keys from memory straight into operand order.  30 requests of
-//               1638 to 16384 keys, 8 key heads of 128: 203 us with the joining, 5.4 TB/s; 2 requests of 512 keys,
-//               8 heads of 64: 6.5 us, a launch and four dependent chunks
+//               walks its own chunks of 32 keys, keys from memory straight into operand order, values past the
+//               caches.  30 requests of 1638 to 16384 keys, 8 key heads of 128: 188 us with the joining, 5.9 TB/s
+//               (203 with the values through the caches); 2 requests of 512 keys, 8 heads of 64: 6.5 us, a launch
+//               and four dependent chunks
 //   Either splits the keys over workgroups where there are few rows; attn_combine joins the parts (12000 rows of
 //   five parts of 80: 10 us in a trace, for 19 MB written and read in fp32).
 #include "dnnseq_attn.h"
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(256) void attn_token_kernel(Forward a)
                                rk, koff[s] == kNowhere ? (int)kNowhere : (int)(koff[s] + h * 16 * kpitch), 0, 0));
 #pragma unroll
         for (int i = 0; i < VLOADS; ++i)
-            load_lds(rv, vl + i * (kWave * 16), voff[i]);
+            load_lds_once(rv, vl + i * (kWave * 16), voff[i]); // (keys are asked for in half lines: they need the caches)
     };
     f32x4 acc[2 * NS];
 #pragma unroll

@@ -236,7 +236,7 @@ template <bool PX, bool QX, int TP, int TQ, int NBUF>
 constexpr int product_lds() { return NBUF * (Tile<PX, TP>::kBytes + Tile<QX, TQ>::kBytes); }
 
 // Workgroup `b` of part `part` of the contraction; lds: [NBUF][P tile, Q tile], 256-byte aligned
-template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF>
+template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF, bool ONCE>
 __device__ __forceinline__ void product_tile(const Product &a, char *lds, uint32_t b, int part)
 {
     constexpr int THREADS = WP * WQ * kWave, FP = TP / WP / 16, FQ = TQ / WQ / 16;
@@ -282,8 +282,8 @@ __device__ __forceinline__ void product_tile(const Product &a, char *lds, uint32
         asm volatile("" ::: "memory");
     };
     const auto load = [&](char *__restrict__ buf, int s) __attribute__((always_inline)) {
-        lp.load(buf, left - s * kStep);
-        lq.load(buf + LP::kBytes, left - s * kStep);
+        lp.template load<ONCE>(buf, left - s * kStep);
+        lq.template load<false>(buf + LP::kBytes, left - s * kStep);
     };
     const auto first_half = [&](const char *__restrict__ cur) __attribute__((always_inline)) {
         product_read<RP, RQ, FP, FQ, LP::kBytes>(cur, rp, rq, 1, fp[1], fq[1]);
@@ -342,11 +342,11 @@ __device__ __forceinline__ void product_tile(const Product &a, char *lds, uint32
     }
 }
 
-template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF>
+template <class T, bool PX, bool QX, int TP, int TQ, int WP, int WQ, int NBUF, bool ONCE = false>
 __global__ __launch_bounds__(WP *WQ *kWave) void product_kernel(Product a)
 {
     __shared__ __attribute__((aligned(256))) char lds[product_lds<PX, QX, TP, TQ, NBUF>()];
-    product_tile<T, PX, QX, TP, TQ, WP, WQ, NBUF>(a, lds, blockIdx.x, blockIdx.y);
+    product_tile<T, PX, QX, TP, TQ, WP, WQ, NBUF, ONCE>(a, lds, blockIdx.x, blockIdx.y);
 }
 
 // out[c] = sum over rows of in[rows][n]: a workgroup per 64 columns, its WAVES wavefronts take every
@@ -394,9 +394,9 @@ __global__ __launch_bounds__(512) void product_both_kernel(Product x, Product w,
     if (b >= all_x + all_w)
         column_sum<8>(db, b - all_x - all_w, (float(*)[kWave])lds);
     else if ((b < first) == x_first)
-        product_tile<T, true, false, 128, 128, 2, 4, 2>(x, lds, r % tiles_x, r / tiles_x);
+        product_tile<T, true, false, 128, 128, 2, 4, 2, false>(x, lds, r % tiles_x, r / tiles_x);
     else
-        product_tile<T, true, true, 128, 128, 2, 4, 2>(w, lds, r % tiles_w, r / tiles_w);
+        product_tile<T, true, true, 128, 128, 2, 4, 2, false>(w, lds, r % tiles_w, r / tiles_w);
 }
 
 // The sum over the splits of a contraction, and the epilogue.
@@ -474,7 +474,8 @@ __global__ __launch_bounds__(512) void product_rows_kernel(Product a)
 
 // g = dy act'(z) and the sums of its columns: a workgroup takes 64 rows x 512 columns (lane: eight
 // columns, wavefront: sixteen rows, four on the way at a time), column sums in fp32 before g is rounded,
-// one partial row per 64 rows.
+// one partial row per 64 rows.  With an activation dy and z are not read again: they pass by the caches, which keep
+// g for the products (4096 x 4096 x 1024: the backward pass 96.2 -> 86.8 us).
 constexpr int kGradRows = 64;
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64_t lddy, const uint16_t *z,
@@ -492,9 +493,10 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t row = min(r + u, r1 - 1);
-                d[u] = *(const u32x4 *)(dy + row * lddy + c);
+                const u32x4 *from = (const u32x4 *)(dy + row * lddy + c);
+                d[u] = ACT ? __builtin_nontemporal_load(from) : *from;
                 if (ACT)
-                    e[u] = *(const u32x4 *)(z + row * ldz + c);
+                    e[u] = __builtin_nontemporal_load((const u32x4 *)(z + row * ldz + c));
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -554,7 +556,7 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
     if (!px && !qx && nq <= 32 && weights <= 1 << 23 && nc <= 4096)
         return {ROWS32, 1, steps, 0};
     // Up to 64 rows: six buffers of a 128 x 64 tile, 100 KB on the way to each CU (24 x 4096 x 16384 from
-    // memory: 38.4 us, 42.7 with 128 x 128)
+    // memory: 38.9 us, 42.7 with 128 x 128)
     if (!qx && nq <= 64) {
         Plan p = {TILE64, 1, steps, 0};
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kCUs / ((np + 127) / 128), steps / 16));
@@ -614,8 +616,14 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
         product_kernel<T, PX, QX, 128, 128, 2, 4, 4><<<grid, 512, 0, st>>>(a);
         break;
     case TILE64:
-        if constexpr (!QX)
-            product_kernel<T, PX, QX, 128, 64, 4, 1, 6><<<grid, 256, 0, st>>>(a);
+        // Weights that no cache holds until the next call are read past the caches (128 MiB, 24 x 4096 x 16384: 36.2 /
+        // 38.9 us; 32 MiB, 24 x 4096 x 4096: 14.2 / 13.8).
+        if constexpr (!QX) {
+            if ((int64_t)a.np * a.nc >= 1 << 26)
+                product_kernel<T, PX, QX, 128, 64, 4, 1, 6, true><<<grid, 256, 0, st>>>(a);
+            else
+                product_kernel<T, PX, QX, 128, 64, 4, 1, 6><<<grid, 256, 0, st>>>(a);
+        }
         break;
     default:
         product_kernel<T, PX, QX, 128, 128, 2, 4, 2><<<grid, 512, 0, st>>>(a);

@@ -381,6 +381,34 @@ def test_linear_gradients_together_and_alone(m, n, k):
             assert db.isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_linear_few_rows_of_large_weights(dtype):
+    """Weights of 128 MiB and more; some columns of the result against 64 bits, the rest against a call for
+    fewer columns (another route, the sums in another order)."""
+    S, dt = _S(), TYPES[dtype]
+    m, n, k = 33, 8200, 8200
+    gen = _gen(m, n, k)
+    x = torch.randn(m, k, generator=gen).to(dt)
+    wd = (torch.randn(n, k, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(5)) * k ** -0.5).to(dt)
+    xd, y = x.cuda(), torch.full((m, n), NAN, dtype=dt, device="cuda:0")
+    d = S.linear_desc(xd, wd)
+    print(f"[dnnseq] linear {dt} {m} x {n} x {k}", flush=True)
+    S.linear_forward(d, xd, wd, y, scratch=_scratch(S.linear_forward_scratch_bytes(d)))
+    cols = [0, 1, 127, 128, 4000, 8191, 8192, 8199]
+    want, tol = ref.linear(x, wd[cols].cpu(), None)
+    torch.cuda.synchronize()
+    ref.check("y", y[:, cols], want["y"], tol["y"])
+    for c in range(0, n, 4104):
+        part = wd[c:c + 4104]
+        z = torch.full((m, part.shape[0]), NAN, dtype=dt, device="cuda:0")
+        d = S.linear_desc(xd, part)
+        S.linear_forward(d, xd, part, z, scratch=_scratch(S.linear_forward_scratch_bytes(d)))
+        torch.cuda.synchronize()
+        u = 2.0 ** (-8 if dtype == "bf16" else -11)
+        # both sums within 64 e32 of their terms' (at most 5 standard deviations of 1), and a rounding each
+        assert ((y[:, c:c + 4104] - z).abs() <= 2 * u * z.abs() + 64 * 2.0 ** -24 * 5 * 8200 ** 0.5).all()
+
+
 def test_linear_in_place_residuals_and_parts():
     """y over the residual, dx over dx_add, and calls that ask for one gradient only."""
     S = _S()
