@@ -457,7 +457,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
         d[i] = own_fragment(drow, in, a.dim, i);
         delta += dot8<T>(d[i], own_fragment(orow, in, a.dim, i));
     }
-    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e, minus = -halves_sum(delta);
+    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    float minus = -halves_sum(delta);
     float rest = 0.f;
     Load lk, lv;
     lk.init(a.k + row_offset(a.sk, b, g, 0), a.sk.token, a.dim);
@@ -470,6 +471,23 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
 #pragma unroll
     for (int e = 0; e < NS; ++e)
         dq[e] = f32x16{};
+    const auto sum_p_dp = [&](const char *__restrict__ cur) __attribute__((always_inline)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int block = 0; block < 2; ++block) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int i = 0; i < 2 * NS; ++i) {
+                s = T::mma32(along.get(cur, block, i), q[i], s);
+                dp = T::mma32(along.get(cur + Load::kBytes, block, i), d[i], dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * block + 8 * (i / 4) + i % 4 < limit - 4 * half)
+                    sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)), dp[i], sum);
+        }
+        return halves_sum(sum);
+    };
     const auto step = [&](const char *__restrict__ cur, char *__restrict__ nxt, int key0) __attribute__((always_inline)) {
         lk.load(nxt, key0 + kTileRows, kl); // (past the end: zeros, no memory is read)
         lv.load(nxt + Load::kBytes, key0 + kTileRows, kl);
@@ -514,6 +532,13 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(Backward a)
     if (0 < end) {
         lk.load(lds, 0, kl);
         lv.load(lds + Load::kBytes, 0, kl);
+        __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the first tile has landed
+        __syncthreads();                    // and everyone's
+        // Rows with no more keys than that tile: delta from p and dp themselves.  What the rounding of o puts into it
+        // would be left in dq, most with few keys (two keys, bf16: error of dq 0.0046 of its norm).
+        const int last_own = min(r0 + w * 32 + 32, ql * a.group) - 1;
+        if (last_own >= r0 + w * 32 && limit_of(last_own) <= kTileRows)
+            minus = -sum_p_dp(lds);
         for (int k0 = 0, turn = 0; k0 < end; k0 += kTileRows, turn ^= 1) {
             __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0): this wavefront's part of the tile has landed
             __syncthreads();                    // and everyone's; the other buffer is no longer read

@@ -257,6 +257,33 @@ def test_attention_gradient_against_differences():
         assert abs(got - diff) <= float((tol[name] * way.abs()).sum()) + 1e-6 * float(way.abs().sum()), (name, got, diff)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("length,causal", [(2, False), (3, True), (5, False), (17, True), (64, False)])
+def test_attention_gradients_of_few_keys(dtype, length, causal):
+    """With few keys ds is a difference of nearly equal numbers, and the rounding of o would show in dq: all of
+    dq's error together is that of its own rounding, and as much again."""
+    S, gen, dt = _S(), _gen(length), TYPES[dtype]
+    B, H, D = 16, 8, 64
+    q, k, v, dout = (torch.randn(B, H, length, D, generator=gen).to(dt) for _ in range(4))
+    x = [t.double().requires_grad_() for t in (q, k, v)]
+    s = x[0] @ x[1].transpose(2, 3) * D ** -0.5
+    if causal:
+        s = s.masked_fill(torch.ones(length, length).triu(1).bool(), -math.inf)
+    (torch.softmax(s, -1) @ x[2] * dout.double()).sum().backward()
+    qd, kd, vd, doutd = q.cuda(), k.cuda(), v.cuda(), dout.cuda()
+    o, dq, dk, dv = (torch.full_like(qd, NAN) for _ in range(4))
+    lse = torch.empty(B, H, length, device="cuda:0")
+    d = S.attention_desc(qd, kd, vd, o, causal=causal)
+    print(f"[dnnseq] attention {dt} of {length} keys", flush=True)
+    S.attention_forward(d, qd, kd, vd, o, lse=lse, scratch=_scratch(S.attention_forward_scratch_bytes(d)))
+    S.attention_backward(d, qd, kd, vd, o, doutd, lse, dq, dk, dv, _scratch(S.attention_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    # a rounding's deviation: at most u / sqrt 3 of an element (u: half a unit in the last place, at a binade's lower end)
+    u = 2.0 ** (-8 if dtype == "bf16" else -11)
+    err = (dq.double().cpu() - x[0].grad).norm() / x[0].grad.norm()
+    assert float(err) <= 2 ** 0.5 * u / 3 ** 0.5, float(err)
+
+
 def test_attention_many_heads():
     """More (request, head) pairs than 16 bits count."""
     S, gen, dt = _S(), _gen(77), torch.bfloat16
