@@ -7,12 +7,13 @@
 // written once by an elementwise pass that also sums db, in the type of the tensors: the matrix
 // cores take 16-bit operands, so it is rounded where any of its uses would round it.
 //
-// What bounds it: 8192 x 8192 x 8192 in tiles of 256 x 256, 770 us, 1.42 PFLOP/s: the matrix units are busy for 74 %
-// of the cycles at 1.83 GHz, the rest goes to the barrier of each step and to the operands' first reads behind it.
-// Short contractions add the epilogue, which nothing overlaps with one tile to a CU (4096 x 4096 x 1024 with GELU and z
-// kept: 41.5 us, 24 of them the steps, 67 MB of results).  Up to 64 rows: reading the weights (24 x 4096 x
-// 16384 39 us, 3.5 TB/s).  One row: a launch and the workgroups' first reads (1 x 4096 x 1024 4.7 us).
-// act_grad: memory, 100 MB in 20 us, 5 TB/s.
+// What bounds it: 8192 x 8192 x 8192 in tiles of 256 x 256, 770 us, 1.42 PFLOP/s: the matrix units are busy for 70-74 %
+// of the cycles, and the clock gives way to the power drawn (a step takes 1.06 us with one tile on the chip, 1.5 on all
+// CUs, 1.2 there with zeros as data).  Short contractions add the epilogue, which nothing overlaps with one tile to a
+// CU (4096 x 4096 x 1024 with GELU and z kept: 41 us, 24 of them the steps, 67 MB of results).  Gradients of the same: 82 us, 1.1
+// PFLOP/s in both products' launch (60 us), act_grad 20 (100 MB, 5 TB/s, vector units 77 % busy).  Up to 64 rows:
+// reading the weights (24 x 4096 x 16384 36 us, 4.6 TB/s without joining the parts).  One row: a launch and the
+// workgroups' first reads (1 x 4096 x 1024 4.7 us).
 #include "dnnseq_gemm.h"
 #include "dnnseq_launch.h"
 
@@ -381,22 +382,22 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(Columns a)
     column_sum<16>(a, blockIdx.x, red);
 }
 
-// Both products of a backward pass in one launch, two workgroups to a CU: what one of them waits for, the
-// other multiplies through (4096 x 4096 x 1024: 42 + 42 us apart, 68 here).  `x` has tiles_x tiles in parts_x parts, `w` likewise;
-// the longer workgroups come first.  The last workgroups add up the partial rows of db, a launch less.
-template <class T>
+// Both products of a backward pass in one launch: apart, neither fills the CUs with large tiles.  `x` has tiles_x
+// tiles in all_x / tiles_x parts, `w` likewise; the longer workgroups come first.  The last workgroups add up the
+// partial rows of db, a launch less.
+template <class T, int TP, int TQ, int WP, int WQ, int NBUF>
 __global__ __launch_bounds__(512) void product_both_kernel(Product x, Product w, uint32_t tiles_x, uint32_t all_x,
                                                            uint32_t tiles_w, uint32_t all_w, Columns db)
 {
-    __shared__ __attribute__((aligned(256))) char lds[product_lds<true, true, 128, 128, 2>()];
+    __shared__ __attribute__((aligned(256))) char lds[product_lds<true, true, TP, TQ, NBUF>()];
     const bool x_first = x.steps >= w.steps;
     const uint32_t b = blockIdx.x, first = x_first ? all_x : all_w, r = b < first ? b : b - first;
     if (b >= all_x + all_w)
         column_sum<8>(db, b - all_x - all_w, (float(*)[kWave])lds);
     else if ((b < first) == x_first)
-        product_tile<T, true, false, 128, 128, 2, 4, 2, false>(x, lds, r % tiles_x, r / tiles_x);
+        product_tile<T, true, false, TP, TQ, WP, WQ, NBUF, false>(x, lds, r % tiles_x, r / tiles_x);
     else
-        product_tile<T, true, true, 128, 128, 2, 4, 2, false>(w, lds, r % tiles_w, r / tiles_w);
+        product_tile<T, true, true, TP, TQ, WP, WQ, NBUF, false>(w, lds, r % tiles_w, r / tiles_w);
 }
 
 // The sum over the splits of a contraction, and the epilogue.
@@ -534,7 +535,7 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const uint16_t *dy, int64
 constexpr int kCUs = 256;
 
 // Tile and split of a contraction.
-enum { ROWS16, ROWS32, TILE256, TILE128, TILE128_PAIR, TILE64 };
+enum { ROWS16, ROWS32, TILE256, TILE256_128, TILE128, TILE128_PAIR, TILE64 };
 struct Plan {
     int form, splits, steps; // steps per split
     double time;             // us, as estimated
@@ -567,13 +568,15 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
     }
     const int64_t t256 = (int64_t)((np + 255) / 256) * ((nq + 255) / 256);
     const int64_t t128 = (int64_t)((np + 127) / 128) * ((nq + 127) / 128);
+    const int64_t twide = (int64_t)((np + 255) / 256) * ((nq + 127) / 128);
     // Time of a step over all tiles in us, by what was measured: a 256 x 256 tile 1.5 (one workgroup per
-    // CU), a 128 x 128 tile 0.49 alone on a CU with its four buffers, two of them with two buffers each
-    // 1.0.
+    // CU), a 256 x 128 tile 0.83 (three buffers), a 128 x 128 tile 0.49 alone on a CU with its four buffers, two of
+    // them with two buffers each 1.0 (m x n x k, us in 256 x 128 tiles / in the best of the others: 4096 x 2048 x 1024 25.0 /
+    // 30.0, 8192 x 1024 x 4096 64.6 / 80.4, 6000 x 4096 x 2048 105 / 120, 4096 x 4096 x 1024 43.3 / 38.7, 4096 x 1024 x 1024 20.9 / 14.4).
     const double big = 1.5 * (double)((t256 + kCUs - 1) / kCUs), one = 0.49 * (double)((t128 + kCUs - 1) / kCUs),
-                 pair = std::max(1.0, (double)t128 / (2 * kCUs) + 0.3);
+                 wide = 0.83 * (double)((twide + kCUs - 1) / kCUs), pair = std::max(1.0, (double)t128 / (2 * kCUs) + 0.3);
     Plan p = {TILE256, 1, steps, big * steps};
-    if (one <= big && one <= pair) {
+    if (one <= big && one <= pair && one <= wide) {
         p.form = TILE128;
         // idle CUs take parts of the contraction, no shorter than 16 steps: adding the parts up costs a
         // launch and their traffic (128 x 4096 x 4096: 28.8 us in one, 16.9 in four, 19.5 in eight)
@@ -581,7 +584,9 @@ Plan plan_product(int np, int nq, int nc, bool px, bool qx)
         p.steps = std::max(1, (steps + p.splits - 1) / p.splits);
         p.splits = std::max(1, (steps + p.steps - 1) / p.steps);
         p.time = one * p.steps + adding_up(np, nq, p.splits);
-    } else if (pair < big)
+    } else if (wide <= big && wide <= pair)
+        p.form = TILE256_128, p.time = wide * steps;
+    else if (pair < big)
         p.form = TILE128_PAIR, p.time = pair * steps;
     return p;
 }
@@ -599,8 +604,8 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
     const Plan p = plan_product(a.np, a.nq, a.nc, PX, QX);
     a.steps = p.steps;
     a.partial = p.splits > 1 ? scratch : nullptr;
-    const int tile = p.form == TILE256 ? 256 : 128;
-    const int rows = p.form == TILE64 ? 64 : tile;
+    const int tile = p.form == TILE256 || p.form == TILE256_128 ? 256 : 128;
+    const int rows = p.form == TILE256 ? 256 : p.form == TILE64 ? 64 : 128;
     const dim3 grid(((a.np + tile - 1) / tile) * ((a.nq + rows - 1) / rows), p.splits);
     switch (p.form) {
     case ROWS16:
@@ -611,6 +616,9 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
         break;
     case TILE256:
         product_kernel<T, PX, QX, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+        break;
+    case TILE256_128:
+        product_kernel<T, PX, QX, 256, 128, 4, 2, 3><<<grid, 512, 0, st>>>(a);
         break;
     case TILE128:
         product_kernel<T, PX, QX, 128, 128, 2, 4, 4><<<grid, 512, 0, st>>>(a);
@@ -639,12 +647,12 @@ size_t product_scratch(int np, int nq, int nc, bool px, bool qx)
     return s > 1 ? (size_t)s * np * nq * 4 : 0;
 }
 
-// Steps until workgroups of two lengths, the longer ones first, have left the places of two per CU.
-double packed(int64_t n1, int len1, int64_t n2, int len2)
+// Steps until workgroups of two lengths, the longer ones first, have left that many places.
+double packed(int64_t places, int64_t n1, int len1, int64_t n2, int len2)
 {
     if (len1 < len2)
         std::swap(n1, n2), std::swap(len1, len2);
-    const int64_t places = 2 * kCUs, late = n1 % places; // places that are one round of long ones behind
+    const int64_t late = n1 % places; // places that are one round of long ones behind
     double a = (double)(n1 / places) * len1, b = late ? a + len1 : a;
     const int64_t rounds = std::max<int64_t>(0, n2 / places - 4 - len1 / len2); // (whole rounds from the start)
     n2 -= rounds * places;
@@ -659,23 +667,28 @@ double packed(int64_t n1, int len1, int64_t n2, int len2)
     return end + (double)rounds * len2;
 }
 
-// Both products of a backward pass in one launch of 128 x 128 tiles?
+// Both products of a backward pass in one launch, in tiles of 128 x 128, two to a CU, or 256 x 128, one with
+// three buffers?  Estimated like the forms of a single product (m x n x k, us apart / narrow / wide: 200 x 200 x 200
+// 18.9 / 11.0 / 13.3, 4096 x 512 x 512 33.2 / 23.3 / 25.3, 2048 x 2048 x 2048 52.3 / 43.6 / 40.5, 4096 x 2048 x 2048 90.8 / 77.3 /
+// 69.3, 8192 x 4096 x 1024 168 / 146 / 128, 4096 x 4096 x 4096 220 / 283 / 246).
 struct Both {
-    bool taken;
+    bool taken, wide;
     uint32_t tiles_x, tiles_w;
     int steps_x, steps_w, parts_x, parts_w; // steps of a part
     size_t partial_w, total;                // scratch: where the weight gradient's parts begin, all of it
+    double time;                            // us, as estimated
 };
-Both plan_both(const dnnseq_linear_desc &d)
+Both plan_both(const dnnseq_linear_desc &d, bool wide)
 {
     Both b = {};
-    if (!d.m)
-        return b;
-    const auto tiles = [](int v) { return (v + 127) / 128; };
-    b.tiles_x = tiles(d.k) * tiles(d.m), b.tiles_w = tiles(d.k) * tiles(d.n);
-    const int sx = (d.n + kStep - 1) / kStep, sw = (d.m + kStep - 1) / kStep;
+    b.wide = wide;
+    const int places = wide ? kCUs : 2 * kCUs;
+    const auto tiles = [](int v, int size) { return (v + size - 1) / size; };
+    const int across = tiles(d.k, wide ? 256 : 128);
+    b.tiles_x = across * tiles(d.m, 128), b.tiles_w = across * tiles(d.n, 128);
+    const int sx = tiles(d.n, kStep), sw = tiles(d.m, kStep);
     // no part much longer than what every place would have
-    const double each = ((double)b.tiles_x * sx + (double)b.tiles_w * sw) / (2 * kCUs);
+    const double each = ((double)b.tiles_x * sx + (double)b.tiles_w * sw) / places;
     const auto part = [&](int steps, int &parts, int &len) {
         parts = std::max(1, std::min((int)(steps / std::max(each, 8.0) + 0.5), steps / 8));
         len = (steps + parts - 1) / parts;
@@ -685,10 +698,19 @@ Both plan_both(const dnnseq_linear_desc &d)
     part(sw, b.parts_w, b.steps_w);
     b.partial_w = b.parts_x > 1 ? (size_t)b.parts_x * d.k * d.m * 4 : 0;
     b.total = b.partial_w + (b.parts_w > 1 ? (size_t)b.parts_w * d.k * d.n * 4 : 0);
-    const double t = 6 + 1.05 * packed((int64_t)b.tiles_x * b.parts_x, b.steps_x, (int64_t)b.tiles_w * b.parts_w, b.steps_w) +
-                     adding_up(d.k, d.m, b.parts_x) + adding_up(d.k, d.n, b.parts_w);
+    b.time = (wide ? 9.5 : 6) + (wide ? 0.83 : 1.05) * packed(places, (int64_t)b.tiles_x * b.parts_x, b.steps_x,
+                                               (int64_t)b.tiles_w * b.parts_w, b.steps_w) +
+             adding_up(d.k, d.m, b.parts_x) + adding_up(d.k, d.n, b.parts_w);
+    return b;
+}
+Both plan_both(const dnnseq_linear_desc &d)
+{
+    if (!d.m)
+        return {};
+    const Both narrow = plan_both(d, false), wide = plan_both(d, true);
+    Both b = wide.time < narrow.time ? wide : narrow;
     const Plan x = plan_product(d.k, d.m, d.n, true, false), w = plan_product(d.k, d.n, d.m, true, true);
-    b.taken = t < x.time + w.time + 16;
+    b.taken = b.time < x.time + w.time + 18;
     return b;
 }
 
@@ -700,7 +722,11 @@ hipError_t launch_both(Product x, Product w, const Columns &db, const Both &b, f
     w.partial = b.parts_w > 1 ? (float *)((char *)scratch + b.partial_w) : nullptr;
     const uint32_t all_x = b.tiles_x * b.parts_x, all_w = b.tiles_w * b.parts_w;
     const uint32_t sums = db.out ? (db.n + kWave - 1) / kWave : 0;
-    product_both_kernel<T><<<all_x + all_w + sums, 512, 0, st>>>(x, w, b.tiles_x, all_x, b.tiles_w, all_w, db);
+    const auto launch = [&](auto kernel) { kernel<<<all_x + all_w + sums, 512, 0, st>>>(x, w, b.tiles_x, all_x, b.tiles_w, all_w, db); };
+    if (b.wide)
+        launch(product_both_kernel<T, 256, 128, 4, 2, 3>);
+    else
+        launch(product_both_kernel<T, 128, 128, 2, 4, 2>);
     if (b.parts_x > 1)
         launch_finish<T>(x, b.parts_x, st);
     if (b.parts_w > 1)

@@ -365,6 +365,12 @@ def test_linear_shapes(dtype, m, n, k):
     _linear(TYPES[dtype], m, n, k, "gelu", residual=m % 2 == 0, bias=m % 3 != 0, pad=16 * (m % 2), dx_add=m % 2 == 1)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(3000, 2056, 264), (1030, 6152, 136), (2300, 264, 2056)])
+def test_linear_wide_results(dtype, m, n, k):
+    _linear(TYPES[dtype], m, n, k, "mish", residual=True, pad=8, dx_add=True)
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 2048, 4096), (48, 1024, 8192), (2049, 256, 264), (4100, 72, 136)])
 def test_linear_long_contractions(m, n, k):
     _linear(torch.bfloat16, m, n, k, "none", dw_fp32=True)
