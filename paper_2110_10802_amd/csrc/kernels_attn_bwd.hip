@@ -175,8 +175,8 @@ __device__ __forceinline__ void load_floats(const float *p, char *lds)
 // half of the next one's; each phase reads the other's operands from LDS.  Three buffers: a tile is read
 // first one step before its own.  2 x 16 heads x 4093 x 128, causal: 318 us; 474 with the phases one after the
 // other, 324 with all of p and ds in one phase.
-template <class T, int NS, bool CAUSAL>
-__global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward a)
+template <class T, int NS, bool CAUSAL, bool FINE>
+__global__ __launch_bounds__(256, NS > 2 || FINE ? 1 : 2) void attn_dkv_kernel(Backward a)
 {
     constexpr int RS = NS > 2 ? 128 : 64, KEYS = 128;
     typedef TileLoader<RS, 256> Load;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward 
                 de[4 * i + j] = v[j];
         }
     };
-    u32x4 p[2], ds[2]; // rounded to the operands' type
+    u32x4 p[2], ds[2], p_rest[2], ds_rest[2]; // rounded to the operands' type; FINE: what that takes from them
     // Element n of a block's p and ds, those of p[0] and ds[0] first; with the odd ones a pair is packed.
     const auto weight = [&](int block, int n, int t0) __attribute__((always_inline)) {
         const int r = n % 8 / 4 * 8 + n / 8 * 4 + n % 4;
@@ -277,8 +277,13 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward 
         if (T::kHalf)
             dp[block][r] *= c;
         if (n % 2) {
-            p[half_of(r)][pair_of(r)] = T::pack(s[block][r - 1], s[block][r]);
-            ds[half_of(r)][pair_of(r)] = T::pack(dp[block][r - 1], dp[block][r]);
+            const int h = half_of(r), n2 = pair_of(r);
+            p[h][n2] = T::pack(s[block][r - 1], s[block][r]);
+            ds[h][n2] = T::pack(dp[block][r - 1], dp[block][r]);
+            if (FINE) {
+                p_rest[h][n2] = T::pack(s[block][r - 1] - T::lo(p[h][n2]), s[block][r] - T::hi(p[h][n2]));
+                ds_rest[h][n2] = T::pack(dp[block][r - 1] - T::lo(ds[h][n2]), dp[block][r] - T::hi(ds[h][n2]));
+            }
         }
     };
     // Operand j of 4 NS: along for the scores, across for the sums.
@@ -301,6 +306,10 @@ __global__ __launch_bounds__(256, NS > 2 ? 1 : 2) void attn_dkv_kernel(Backward 
             dk[e] = T::mma32(xq[h][e], ds[h], dk[e]);
         else
             dv[e] = T::mma32(xd[h][e], p[h], dv[e]);
+        if (FINE && j % 2)
+            dk[e] = T::mma32(xq[h][e], ds_rest[h], dk[e]);
+        else if (FINE)
+            dv[e] = T::mma32(xd[h][e], p_rest[h], dv[e]);
     };
     const auto landed = [] __attribute__((always_inline)) {
         asm volatile("" ::: "memory");
@@ -597,10 +606,15 @@ hipError_t backward(const Backward &a, hipStream_t st)
     if (a.q_len)
         attn_dq_kernel<T, NS><<<grid_of(a.q_order), 256, 0, st>>>(a);
     if (a.kv_len) {
-        if (a.causal)
-            attn_dkv_kernel<T, NS, true><<<grid_of(a.kv_order), 256, 0, st>>>(a);
+        const auto launch = [&](auto kernel) { kernel<<<grid_of(a.kv_order), 256, 0, st>>>(a); };
+        // FINE: p and ds in two halves, as attn_dq has ds.  Over many rows their roundings average out to as much as
+        // the result's own; over a few, one rounding may be most of the error (20 x 8 heads x 2, bf16: error of dk
+        // 0.0028 of its norm, 0.0016).  There it costs nothing (8 x 8 heads x 2 x 64, forward and backward: 21.1 /
+        // 21.0 us); 64 x 16 x 16 x 64 would be 31.7 -> 40.4, one workgroup to a CU.
+        if (a.q_len <= 64 && (int64_t)a.batch * a.q_heads * a.q_len <= 2048)
+            a.causal ? launch(attn_dkv_kernel<T, NS, true, true>) : launch(attn_dkv_kernel<T, NS, false, true>);
         else
-            attn_dkv_kernel<T, NS, false><<<grid_of(a.kv_order), 256, 0, st>>>(a);
+            a.causal ? launch(attn_dkv_kernel<T, NS, true, false>) : launch(attn_dkv_kernel<T, NS, false, false>);
         if (a.head_splits > 1) {
             const size_t units = (size_t)a.batch * a.kv_heads * a.kv_len * a.dim / 8;
             attn_dkv_sum_kernel<T><<<dim3((unsigned)((units + 255) / 256), 2), 256, 0, st>>>(a);
@@ -645,7 +659,8 @@ hipError_t launch_attention_backward(const dnnseq_attention_desc &d, const void 
     a.sq = d.q, a.sk = d.k, a.sv = d.v, a.so = d.o, a.sdo = d.dout, a.sdq = d.dq, a.sdk = d.dk, a.sdv = d.dv;
     a.batch = d.batch, a.q_heads = d.q_heads, a.kv_heads = d.kv_heads, a.group = d.q_heads / d.kv_heads;
     a.q_len = d.q_len, a.kv_len = d.kv_len, a.dim = d.head_dim, a.causal = d.causal;
-    a.scale = d.scale, a.scale2 = d.scale * kLog2e;
+    a.scale = d.kv_len == 1 ? 0.f : d.scale; // one key: p = 1 whatever q and k are, dq and dk are zero
+    a.scale2 = d.scale * kLog2e;
     const int64_t units = (int64_t)d.batch * d.kv_heads;
     a.q_order = make_groups(units, ((int64_t)d.q_len * a.group + 127) / 128);
     a.kv_order = make_groups(units, (int64_t)((d.kv_len + 127) / 128) * l.head_splits);

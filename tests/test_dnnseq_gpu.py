@@ -284,6 +284,21 @@ def test_attention_gradients_of_few_keys(dtype, length, causal):
     assert float(err) <= 2 ** 0.5 * u / 3 ** 0.5, float(err)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_gradients_of_one_key(dtype):
+    """One key: o is its value, dq and dk are zero."""
+    S, gen, dt = _S(), _gen(1), TYPES[dtype]
+    q, k, v, dout = (torch.randn(3, 4, 1, 40, generator=gen).to(dt).cuda() for _ in range(4))
+    o, dq, dk, dv = (torch.full_like(q, NAN) for _ in range(4))
+    lse = torch.empty(3, 4, 1, device="cuda:0")
+    d = S.attention_desc(q, k, v, o)
+    S.attention_forward(d, q, k, v, o, lse=lse, scratch=_scratch(S.attention_forward_scratch_bytes(d)))
+    S.attention_backward(d, q, k, v, o, dout, lse, dq, dk, dv, _scratch(S.attention_backward_scratch_bytes(d)))
+    torch.cuda.synchronize()
+    assert (dq == 0).all() and (dk == 0).all()
+    assert torch.equal(o, v) and torch.equal(dv, dout)
+
+
 def test_attention_many_heads():
     """More (request, head) pairs than 16 bits count."""
     S, gen, dt = _S(), _gen(77), torch.bfloat16
