@@ -2,7 +2,8 @@
 //   p = exp(s - lse), dp = dout v^T, ds = p (dp - delta), delta = rowsum(dout o)
 //   dq = scale ds k,  dk = scale ds^T q,  dv = p^T dout
 // Two passes, each with one owner for every output element, so nothing is added atomically: eight
-// products (ds enters dq in two halves) instead of the five of a single pass.
+// products (ds enters dq in two halves; dk and dv of few rows take p and ds so too) instead of the five of
+// a single pass.
 //
 //   attn_dq     128 rows per workgroup, 32 per wavefront (columns of s^T = k q^T): takes delta from the
 //               rounded o, walks the keys; ds^T is the column operand of dq^T += k^T ds^T.  Leaves delta,
@@ -17,8 +18,8 @@
 // dq 275 us in a trace (1.0 PFLOP/s over its four products), dkv 318 (0.86), the sum 13.5 (5 TB/s).  8 x 16 heads
 // x 512 x 64, 205 to 512 tokens: 26 and 24 us, the start of a workgroup and the chain of its eight steps.
 //
-// fp16 (attn_norm, attn_bound): ds has entries of the size of dp / keys, which fp16 may not hold.  All of them are multiplied
-// by one power of two c, taken from max |dout_i| max |v_j| >= max |dp|, and dq and dk divided by it.
+// fp16 (attn_norm, attn_bound): ds has entries of the size of dp / keys, which fp16 may not hold.  All of them
+// are multiplied by one power of two c, taken from max |dout_i| max |v_j| >= max |dp|, and dq and dk divided by it.
 #include "dnnseq_attn.h"
 #include "dnnseq_launch.h"
 

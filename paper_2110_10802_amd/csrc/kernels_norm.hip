@@ -1,5 +1,5 @@
 // Layer normalisation of 16-bit rows, forward and backward: bound by memory, every tensor read or
-// written once (16384 x 4096, bf16: forward 49 us, 5.5 TB/s; backward with the residual's gradient 110 us, 4.9
+// written once (16384 x 4096, bf16: forward 49 us, 5.5 TB/s; backward with the residual's gradient 98 us, 5.5
 // TB/s); a few rows by the launches (77 x 1001: 5 us each way).
 //
 // A row stays in the registers of TPR threads (NU units of eight elements each, unit u of thread t at
