@@ -624,10 +624,12 @@ hipError_t launch_product(Product a, float *scratch, hipStream_t st)
         product_kernel<T, PX, QX, 128, 128, 2, 4, 4><<<grid, 512, 0, st>>>(a);
         break;
     case TILE64:
-        // Weights that no cache holds until the next call are read past the caches (128 MiB, 24 x 4096 x 16384: 36.2 /
-        // 38.9 us; 32 MiB, 24 x 4096 x 4096: 14.2 / 13.8).
+        // Weights that come from memory are read past the caches (3 GB of weights in turn, past / through them: 24 x
+        // 4096 x 4096 14.3 / 15.0 us, 24 x 6144 x 8192 23.3 / 24.9, 60 x 8192 x 16384 61.8 / 67.5).  Weights that the
+        // 256 MiB beside the memory still hold lose by it (14.2 / 13.8, 40 x 8192 x 8192 33.6 / 26.1): below 64 MiB a
+        // few layers may be all there is.
         if constexpr (!QX) {
-            if ((int64_t)a.np * a.nc >= 1 << 26)
+            if ((int64_t)a.np * a.nc >= 1 << 25)
                 product_kernel<T, PX, QX, 128, 64, 4, 1, 6, true><<<grid, 256, 0, st>>>(a);
             else
                 product_kernel<T, PX, QX, 128, 64, 4, 1, 6><<<grid, 256, 0, st>>>(a);
